@@ -545,6 +545,182 @@ int pyramidkv_compress_model_lanes(const pkv_config* cfg, pkv_lanes* lanes, int3
                                    void* const* workspaces, size_t workspace_bytes, void* stream);
 
 /*
+ * ------------------------------------------------------------------------------------------------------------
+ * A cache that grows behind the compressed prompt.  Section 4.1 uses the kept rows for the inference that follows;
+ * each new token then takes these steps, none of which reads anything back to the host:
+ *   pyramidkv_cache_reserve            once per step: room for the new rows of every layer
+ *   pyramidkv_append_cache             per layer: rotary positions on the new queries and keys, rows into their pages
+ *   pyramidkv_decode_attention_cache   per layer: the new token attends to all rows of its sequence
+ * and pyramidkv_cache_fork / pyramidkv_cache_compact share, free and move pages between steps.  All calls may be
+ * captured into CUDA graphs: lengths, tables and positions are read on the device.
+ *
+ * pkv_cache: the rows of `layers` layers and `batch` sequences in a pool of pages.  A page holds page_size rows of one
+ * KV head, as for pyramidkv_gather_paged.  Row r of head h of sequence b in layer l lies in page
+ * tables[l][b][h][r / page_size] at slot r % page_size, for r < lens[l][b].  Table entries behind a sequence's last page
+ * are neither read nor written, and neither are slots behind its last row.  An entry outside [0, num_pages) is never
+ * turned into an address: its rows are left out and the workspace status word gets bit 2.
+ *   refs counts for each page the table entries that name it (0 = free); a program that deals its pages out itself has
+ *   no use for it and passes NULL, and then cannot call the three page calls.  A page that is named more than once is
+ *   never written by this library's calls as long as its rows are full, which cache_fork sees to.
+ * All arrays are contiguous.  The struct itself is read on the host, during the call.
+ */
+#define PKV_MAX_CACHE_BATCH 1024  /* sequences of a cache */
+typedef struct pkv_cache {
+  void* k_pool;          /* device [num_pages][page_size][d], config dtype, 16-byte aligned */
+  void* v_pool;
+  int32_t* positions;    /* device [num_pages][page_size]: a row's position in its sequence; or NULL */
+  int32_t* tables;       /* device [layers][batch][H_kv][max_pages] */
+  int32_t* lens;         /* device [layers][batch]: rows each head of a sequence holds */
+  int32_t* refs;         /* device [num_pages], or NULL */
+  int32_t num_pages, page_size, layers, batch, max_pages;
+} pkv_cache;
+
+/*
+ * Bytes of workspace that the calls below need for this cache (host only; 0 for an invalid one).  256-byte aligned,
+ * zeroed by the caller once after allocation: besides the status word it holds counters that the calls leave at zero.
+ * It is a workspace of its own: one that pyramidkv_workspace_bytes sized, and other calls scribble on, does not do.  One
+ * workspace serves any number of caches that need no more; a fork into a cache with more sequences needs the larger of
+ * the two sizes.  Calls that share a workspace must be ordered on one stream, replayed graphs included.
+ * pyramidkv_check_status reads its status word.
+ */
+size_t pyramidkv_cache_workspace_bytes(const pkv_config* cfg, const pkv_cache* cache);
+
+/*
+ * Limits of the calls below (PKV_ERR_UNSUPPORTED beyond): 1024 sequences, 2^27 pages, 2^30 rows of a sequence's table,
+ * 65536 blocks of four (more than four query heads to a KV head: eight) query heads in the batch.
+ *
+ * Rotary positions.  Element pairs (x, y) of a row at position p are turned by the angle p * frequency[i] and scaled:
+ *     x' = magnitude * (x cos - y sin),   y' = magnitude * (y cos + x sin),    i = 0 .. rotary_dim / 2 - 1
+ * Pair i is (i, i + rotary_dim / 2) with PKV_ROTARY_HALF and (2 i, 2 i + 1) with PKV_ROTARY_INTERLEAVED; elements from
+ * rotary_dim on are copied.  Angles are formed in 64 bits and reduced before the sine, so that far positions are exact to
+ * the rounding of fp32; the pairs are turned in fp32 and rounded once.
+ *
+ * pyramidkv_rotary_plan (host only) fills a plan: frequency[i] = base^(-2 i / rotary_dim), then
+ *   PKV_ROTARY_SCALE_LINEAR  divided by `factor`
+ *   PKV_ROTARY_SCALE_NTK     of the base  base * factor^(rotary_dim / (rotary_dim - 2))
+ *   PKV_ROTARY_SCALE_LLAMA3  t = original_positions * frequency / (2 pi) turns; kept where t >= high, divided by `factor`
+ *                            where t <= low, blended linearly in t between
+ *   PKV_ROTARY_SCALE_YARN    blended over the pair index between the pairs that make `high` turns (kept, rounded down) and
+ *                            `low` turns (divided by `factor`, rounded up) within original_positions;
+ *                            magnitude = 0.1 ln(factor) + 1 (1 for every other kind)
+ * A caller may fill or change the fields itself (finite frequencies, any finite magnitude).
+ * Errors: INVALID_ARG (rotary_dim odd, < 2 or > 128, base <= 1, factor < 1, for the last two kinds
+ * original_positions < 1 or not 0 < low < high; for NTK rotary_dim 2).
+ */
+#define PKV_ROTARY_HALF 0
+#define PKV_ROTARY_INTERLEAVED 1
+#define PKV_ROTARY_SCALE_NONE 0
+#define PKV_ROTARY_SCALE_LINEAR 1
+#define PKV_ROTARY_SCALE_NTK 2
+#define PKV_ROTARY_SCALE_LLAMA3 3
+#define PKV_ROTARY_SCALE_YARN 4
+typedef struct pkv_rotary {
+  int32_t rotary_dim;      /* even, <= head_dim */
+  int32_t layout;          /* PKV_ROTARY_HALF or PKV_ROTARY_INTERLEAVED */
+  double  magnitude;
+  double  frequency[64];   /* radians per position; the first rotary_dim / 2 are used */
+} pkv_rotary;
+int pyramidkv_rotary_plan(int32_t rotary_dim, int32_t layout, int32_t scaling, double base, double factor,
+                          int32_t original_positions, double low, double high, pkv_rotary* out);
+
+/*
+ * Rotary positions on queries and keys of a prompt or of single tokens, in one launch.
+ *   positions   device int32; token t of sequence b is at positions[b * positions_stride + t] (stride 0: the same for all)
+ *   q, q_out    [batch][H_q][tokens][d] views;  k, k_out  [batch][H_kv][tokens][d]; either pair may have null pointers
+ *               (not both).  An output may be its input (same pointer and strides); otherwise the two must not overlap.
+ *   inverse     non-zero: turned by the negative angle, same magnitude.  That is the transposed map, so it takes the
+ *               gradient of the outputs to the gradient of the inputs; with magnitude 1 it also undoes the rotation.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+int pyramidkv_rotary(const pkv_config* cfg, const pkv_rotary* plan, const int32_t* positions, int64_t positions_stride,
+                     int32_t batch, int32_t tokens, pkv_tensor q, pkv_tensor q_out, pkv_tensor k, pkv_tensor k_out,
+                     int32_t inverse, void* stream);
+
+/*
+ * New rows of one layer into their pages.  Sequence b brings counts[b] tokens, which are its last rows: token t becomes
+ * row lens[layer][b] - counts[b] + t (lens as pyramidkv_cache_reserve left it).  Its key is given its rotary position, key
+ * and value go to their slots, and positions[b][t] to the cache's positions where it has them.
+ *   plan_or_null       NULL: keys and queries are taken as they are
+ *   positions          as for pyramidkv_rotary; may be NULL if there is no plan and the cache has no positions
+ *   q, q_out           [batch][H_q][tokens][d]: rotated on the way, or both null pointers.  q_out may be q.
+ *   k, v               [batch][H_kv][tokens][d]
+ *   counts_or_null     device int32 [batch], taken as if clamped to [0, tokens]; NULL: `tokens` each.  Tokens behind a
+ *                      sequence's count are not read and their places in q_out are left as they were.
+ * A row whose table entry is outside the pool, or that lies outside [0, max_pages * page_size), is left out: status bit 2.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+int pyramidkv_append_cache(const pkv_config* cfg, const pkv_cache* cache, int32_t layer, const pkv_rotary* plan_or_null,
+                           const int32_t* positions, int64_t positions_stride, int32_t tokens, pkv_tensor q, pkv_tensor q_out,
+                           pkv_tensor k, pkv_tensor v, const int32_t* counts_or_null,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Positions of a compressed layer's rows, from the packed index list that pyramidkv_compress_layer_paged wrote beside them,
+ * into positions [num_pages][page_size] at the rows' slots.  Arguments as for pyramidkv_gather_paged.
+ */
+int pyramidkv_cache_positions(const pkv_config* cfg, const int32_t* indices, const int32_t* seq_lens, int32_t batch,
+                              int32_t k_layer, const int32_t* block_table, int32_t page_size, int32_t num_pages,
+                              int32_t* positions, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of one new token per sequence over the rows of one layer.  With s = q . k_r * scale for the query at position
+ * p and row r at position p_r, the logit is
+ *     x = softcap > 0 ? softcap * tanh(s / softcap) : s,   then   x - slope_g * (p - p_r)   where slopes are given,
+ * and with query positions a row is seen if p_r <= p and (window == 0 or p - p_r < window or p_r < prefix).  Without query
+ * positions every row is seen.  out[b][g] is the softmax over the seen rows times V; a query that sees no row (or only rows
+ * whose weights are all zero) gets zeros and -infinity for lse.  Rows that are not seen are not read.
+ *   q               device, head g of sequence b at q.ptr + b * stride_batch + g * stride_head (stride_token is not used)
+ *   out             device [batch][H_q][d] floats;  lse_or_null  device [batch][H_q] floats, the natural logarithm of the
+ *                   sum of exponentials, with which parts of a cache can be joined
+ *   options_or_null NULL: scale 1/sqrt(d), no cap, no bias, every row seen
+ * Sums are formed in fp32; the work is split over the lengths and joined in an order that does not depend on timing, so that
+ * equal calls give equal bits.
+ * Errors: INVALID_ARG (slopes, window or prefix without query positions; query positions without cache positions),
+ * UNSUPPORTED, WORKSPACE, CUDA.
+ */
+typedef struct pkv_attend_options {
+  float scale;                 /* 0: 1 / sqrt(d) */
+  float softcap;               /* 0: none */
+  int32_t window;              /* 0: none */
+  int32_t prefix;              /* rows at positions below it are seen whatever the window */
+  const float* slopes;         /* device [H_q] or NULL */
+  const int32_t* q_positions;  /* device [batch] or NULL */
+} pkv_attend_options;
+int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cache, int32_t layer,
+                                     const pkv_attend_options* options_or_null, pkv_tensor q, float* out, float* lse_or_null,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Pages.  `from` and `to` describe the same pools (equal pool pointers, positions, num_pages and page_size, layers and
+ * max_pages); their tables, lens and refs are either all the same (the cache is changed in place) or all distinct.  Then
+ * `from` is left as it was, except that pages it does not name may hold new rows; from that call on it is `to` that owns
+ * the pool (its refs are the ones that count), and `from` is a record of the past.
+ * All or nothing: where the pool has too few free pages, a sequence would need more than max_pages, or a parent is outside
+ * [-1, batch of from), no page is dealt out or copied, granted is filled with zeros and the status word gets bit 4 (bit 3
+ * for a parent).  In place everything stays as it was; a `to` of its own is not to be used then, `from` is as good as before.
+ *
+ * pyramidkv_cache_fork   sequence c of `to` goes on from sequence parents[c] of `from`, or starts empty for -1: full pages
+ *     are shared; a last page that is not full goes to the parent's first child, and every other child gets a copy of its
+ *     rows; add[l][c] more rows (negative: 0) are made room for.  Pages that no sequence goes on with are freed.  New pages
+ *     are the lowest free ones, in ascending order over (layer, sequence, head, page).
+ *       parents  device int32 [batch of to];  add_or_null, granted_or_null  device int32 [layers][batch of to]; add's layers
+ *       are add_stride entries apart (0: one list for all layers); granted gets the rows made room for
+ * pyramidkv_cache_reserve   the same with every sequence its own parent (equal batches)
+ * pyramidkv_cache_compact   pages in use above the number of pages in use move into the free ones below it: the lowest free
+ *     page takes the lowest of them, and so on.  Tables follow; lens stay.  used_or_null: device int32, the number of pages
+ *     in use; from there on the pool is free.  A page named by tables other than `from`'s must not be in the pool.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+int pyramidkv_cache_fork(const pkv_config* cfg, const pkv_cache* from, const pkv_cache* to, const int32_t* parents,
+                         const int32_t* add_or_null, int64_t add_stride, int32_t* granted_or_null,
+                         void* workspace, size_t workspace_bytes, void* stream);
+int pyramidkv_cache_reserve(const pkv_config* cfg, const pkv_cache* from, const pkv_cache* to,
+                            const int32_t* add, int64_t add_stride, int32_t* granted_or_null,
+                            void* workspace, size_t workspace_bytes, void* stream);
+int pyramidkv_cache_compact(const pkv_config* cfg, const pkv_cache* from, const pkv_cache* to, int32_t* used_or_null,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Test aids; the paper has no counterpart.
  *
  * pyramidkv_test_hooks: process-wide knobs read by the calls that follow.  wait_clocks > 0 replaces the bound
@@ -568,8 +744,9 @@ int pyramidkv_test_slow_copy(void* dst, const void* src, size_t bytes, int32_t s
  * bounded wait or saw an impossible state; *detail_or_null receives the word),
  * or PKV_ERR_CUDA.  Bits of the word: 0 the selection emitted a wrong count,
  * 1 a bounded wait ran out, 2 a block-table entry outside the pool, 3 an index
- * entry outside its sequence.  The bits stay set until the caller zeroes the
- * first 256 bytes of the workspace.
+ * entry outside its sequence (a parent outside the batch), 4 a page call that could
+ * not be met.  The bits stay set until the caller zeroes the first 256 bytes of the
+ * workspace.
  */
 int pyramidkv_check_status(const void* workspace, void* stream, uint32_t* detail_or_null);
 

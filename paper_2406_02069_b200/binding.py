@@ -47,7 +47,9 @@ EXPORTS = ("pyramidkv_strerror", "pyramidkv_layer_budgets", "pyramidkv_kept_coun
            "pyramidkv_lanes_create", "pyramidkv_lanes_destroy", "pyramidkv_lanes_info",
            "pyramidkv_compress_model_lanes", "pyramidkv_test_hooks", "pyramidkv_test_slow_copy",
            "pyramidkv_attend_window", "pyramidkv_attend_compress_layer",
-           "pyramidkv_profile_attend_compress_layer")
+           "pyramidkv_profile_attend_compress_layer", "pyramidkv_cache_workspace_bytes", "pyramidkv_rotary_plan",
+           "pyramidkv_rotary", "pyramidkv_append_cache", "pyramidkv_cache_positions", "pyramidkv_decode_attention_cache",
+           "pyramidkv_cache_fork", "pyramidkv_cache_reserve", "pyramidkv_cache_compact")
 PKV_MAX_STAGES = 8
 
 
@@ -117,8 +119,19 @@ def _load() -> ctypes.CDLL:
     lib.pyramidkv_test_hooks.argtypes = [I64, I32]
     lib.pyramidkv_test_slow_copy.argtypes = [P, P, SZ, I32, P]
     lib.pyramidkv_check_status_static.argtypes = [P, P]
+    F64 = ctypes.c_double
+    lib.pyramidkv_cache_workspace_bytes.argtypes = [CFG, P]
+    lib.pyramidkv_cache_workspace_bytes.restype = SZ
+    lib.pyramidkv_rotary_plan.argtypes = [I32, I32, I32, F64, F64, I32, F64, F64, P]
+    lib.pyramidkv_rotary.argtypes = [CFG, P, P, I64, I32, I32, PkvTensor, PkvTensor, PkvTensor, PkvTensor, I32, P]
+    lib.pyramidkv_append_cache.argtypes = [CFG, P, I32, P, P, I64, I32, PkvTensor, PkvTensor, PkvTensor, PkvTensor, P, P, SZ, P]
+    lib.pyramidkv_cache_positions.argtypes = [CFG, P, P, I32, I32, P, I32, I32, P, P, SZ, P]
+    lib.pyramidkv_decode_attention_cache.argtypes = [CFG, P, I32, P, PkvTensor, P, P, P, SZ, P]
+    lib.pyramidkv_cache_fork.argtypes = [CFG, P, P, P, P, I64, P, P, SZ, P]
+    lib.pyramidkv_cache_reserve.argtypes = [CFG, P, P, P, I64, P, P, SZ, P]
+    lib.pyramidkv_cache_compact.argtypes = [CFG, P, P, P, P, SZ, P]
     for name in EXPORTS:
-        if name not in ("pyramidkv_strerror", "pyramidkv_workspace_bytes"):
+        if name not in ("pyramidkv_strerror", "pyramidkv_workspace_bytes", "pyramidkv_cache_workspace_bytes"):
             getattr(lib, name).restype = ctypes.c_int
     return lib
 
@@ -152,6 +165,8 @@ class _LazyNative:
             module = importlib.util.module_from_spec(spec)
             spec.loader.exec_module(module)
             module.set_config_type(PkvConfig)
+            from . import cache                         # (it imports this module)
+            module.set_cache_types(cache.PkvCache, cache.PkvRotary)
         except (OSError, subprocess.CalledProcessError, ImportError) as e:
             warnings.warn("the native half of the binding is not available (%s): calls take some 20 us more of host time" % e,
                           RuntimeWarning, stacklevel=3)
@@ -165,7 +180,8 @@ class _LazyNative:
 
 
 _NATIVE_CALLS = ("compress_layer", "attend_compress_layer", "compress_layer_paged", "score_window", "select_topk", "gather_compact",
-                 "decode_attention", "decode_attention_paged")
+                 "decode_attention", "decode_attention_paged", "rotary", "append_cache", "decode_attention_cache", "cache_reserve",
+                 "cache_fork", "cache_compact")
 _native = _LazyNative()
 _NOT_TAKEN = -1        # the native call left the arguments to the checks here; nothing was enqueued
 

@@ -14,6 +14,7 @@
 #include "pkv_decode.cuh"
 #include "pkv_extras.cuh"
 #include "pkv_gather.cuh"
+#include "pkv_host.cuh"
 #include "pkv_score_generic.cuh"
 #include "pkv_score_tc.cuh"
 #include "pkv_score_resident.cuh"
@@ -31,7 +32,6 @@ std::atomic<int> g_test_withhold{0};
 std::atomic<int> g_test_withhold_attend{0};  // 1: the withheld K tile, in the window-attention kernel
 std::atomic<int> g_test_two_sweeps{0};     // 1: never take the single-sweep kernel for short contexts
 
-constexpr size_t kAlign = 256;
 constexpr int kPartialChunk = 128;   // keys per partial slot of the fp32-pipe path (sizes the workspace)
 static_assert(kPartialChunk == kGenTile, "one partial per tile");
 // fp32 scores: logits are kept between the passes up to this size.  Scores of 32 / 8 heads, d = 128, 32 window rows, kept
@@ -39,28 +39,6 @@ static_assert(kPartialChunk == kGenTile, "one partial per tile");
 // pipe, 64 / 8 heads x 64 rows in bf16, 16384 tokens (256 MB) 567 / 916.  With few rows and long contexts it is the other way round, because every CTA of the sums
 // merges all partials: 8 rows x 4 heads, 65536 tokens (64 MB) 289 / 266, 131072 715 / 524; d = 64, 32768 85 / 78.
 constexpr size_t kMaxLogitBytes = size_t{256} << 20;
-
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-bool config_ok(const pkv_config* c) {
-  if (!c) return false;
-  if (c->num_layers < 1 || c->num_kv_heads < 1 || c->num_q_heads < 1) return false;
-  if (c->num_q_heads % c->num_kv_heads != 0) return false;
-  if (c->window < 1 || c->avg_budget < c->window) return false;
-  if (c->pool_kernel < 1 || (c->pool_kernel % 2) == 0) return false;
-  if (!(c->beta >= 1.0) || c->beta > 1.0e6) return false;
-  if (c->schedule != PKV_SCHEDULE_LINEAR && c->schedule != PKV_SCHEDULE_GEOMETRIC) return false;
-  if ((c->flags & ~PKV_FLAG_INPUTS_FINAL) != 0 || c->sweep_ctas > 1024) return false;
-  return true;
-}
-
-int config_supported(const pkv_config* c) {
-  if (c->dtype != PKV_DTYPE_FP32 && c->dtype != PKV_DTYPE_BF16 && c->dtype != PKV_DTYPE_FP16)
-    return PKV_ERR_UNSUPPORTED;
-  if (c->head_dim != 64 && c->head_dim != 128) return PKV_ERR_UNSUPPORTED;
-  if (c->pool_kind != PKV_POOL_MAX && c->pool_kind != PKV_POOL_AVG) return PKV_ERR_UNSUPPORTED;
-  return PKV_OK;
-}
 
 // Eq. 1 in integers.  beta = bq / 1024.  With k_total = m (B - alpha):
 //   k^l = k_total * ((2 bq - 1024)(m - 1) - (2 bq - 2048) l) / (bq m (m - 1)),
@@ -219,38 +197,6 @@ int build_table(const pkv_config* c, const int32_t* seq_lens, int batch, int k_l
   return PKV_OK;
 }
 
-// A [batch][heads][token][d] view the kernels can take: 16-byte aligned base and strides, rows that do not
-// overlap, and a positive stride along every dimension that has more than one entry (a broadcast or reversed
-// view has no tensor map and would be mis-sized by the overlap test below).
-bool tensor_ok(const pkv_tensor& t, int d, int elem_bytes, int batch = 1, int heads = 1) {
-  if (!t.ptr || t.stride_token < d) return false;
-  if (reinterpret_cast<uintptr_t>(t.ptr) % 16) return false;
-  if ((batch > 1 && t.stride_batch <= 0) || (heads > 1 && t.stride_head <= 0)) return false;
-  const int64_t q = 16 / elem_bytes;
-  return t.stride_token % q == 0 && t.stride_head % q == 0 && t.stride_batch % q == 0;
-}
-
-TensorView view(const pkv_tensor& t) { return TensorView{t.ptr, t.stride_batch, t.stride_head, t.stride_token}; }
-
-int check_launch() { return cudaPeekAtLastError() == cudaSuccess ? PKV_OK : PKV_ERR_CUDA; }
-
-// Launch with programmatic stream serialisation: the kernel may be scheduled while its predecessor in
-// the stream drains; the kernels order themselves with pdl_wait() (pkv_common.cuh).
-template <typename... KArgs, typename... Args>
-void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
-
 // Optional per-kernel timing (pyramidkv_profile_layer): when armed, an event is recorded after every launch.
 struct StageTimer {
   cudaEvent_t ev[PKV_MAX_STAGES + 1];
@@ -263,49 +209,6 @@ void mark(cudaStream_t st, const char* name) {
   if (!g_timer || g_timer->n >= PKV_MAX_STAGES) return;
   g_timer->name[g_timer->n] = name;
   cudaEventRecord(g_timer->ev[++g_timer->n], st);
-}
-
-// ---------------------------------------------------------------- outputs still in flight
-// The tensor-core sweeps start reading Q and K before the kernels ahead of them in the stream have finished.
-// That is only right for tensors those kernels do not write, so the library remembers where its last calls put
-// K/V rows (packed caches, page pools) and a sweep whose Q or K overlaps one of them waits like any other kernel.
-struct ByteRange { uintptr_t lo, hi; };
-std::mutex g_out_mutex;
-ByteRange g_recent_out[16];
-unsigned g_recent_out_next = 0;
-
-void note_output(const void* ptr, size_t bytes) {
-  if (!ptr || !bytes) return;
-  std::lock_guard<std::mutex> lock(g_out_mutex);
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(ptr);
-  g_recent_out[g_recent_out_next++ % 16] = ByteRange{lo, lo + bytes};
-}
-
-bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {
-  const int64_t last = (batch - 1) * std::max<int64_t>(t.stride_batch, 0) +
-                       (heads - 1) * std::max<int64_t>(t.stride_head, 0) + (tokens - 1) * t.stride_token + d;
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(t.ptr), hi = lo + static_cast<uintptr_t>(last) * elem_bytes;
-  std::lock_guard<std::mutex> lock(g_out_mutex);
-  for (const ByteRange& r : g_recent_out)
-    if (r.hi > r.lo && lo < r.hi && r.lo < hi) return true;
-  return false;
-}
-
-// SMs the persistent score kernels may count on: the device's, or fewer while a call runs them on a lane that
-// owns only a group of the SMs (pyramidkv_compress_model_lanes sets the limit for its own thread).
-thread_local int tl_sm_limit = 0;
-
-int device_sm_count() {
-  static int sms[64] = {};
-  if (tl_sm_limit > 0) return tl_sm_limit;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (!sms[dev]) {
-    int n = 0;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    sms[dev] = n;
-  }
-  return sms[dev];
 }
 
 // ---------------------------------------------------------------- scores
@@ -1427,6 +1330,24 @@ int pyramidkv_gather_paged(const pkv_config* cfg, pkv_tensor k, pkv_tensor v, co
   if (int rc = build_table(cfg, seq_lens, batch, k_layer, &table, &max_n, &rows)) return rc;
   return run_gather_paged(cfg, k, v, indices, table, rows, block_table, page_size, num_pages, k_pool, v_pool,
                           static_cast<uint32_t*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+int pyramidkv_cache_positions(const pkv_config* cfg, const int32_t* indices, const int32_t* seq_lens, int32_t batch,
+                              int32_t k_layer, const int32_t* block_table, int32_t page_size, int32_t num_pages,
+                              int32_t* positions, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!config_ok(cfg) || !indices || !block_table || !positions || page_size < 1 || num_pages < 1) return PKV_ERR_INVALID_ARG;
+  if (int rc = config_supported(cfg)) return rc;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < kAlign) return PKV_ERR_WORKSPACE;
+  CachePositionsParams p{};
+  int max_n;
+  if (int rc = build_table(cfg, seq_lens, batch, k_layer, &p.seq, &max_n, &p.total_rows)) return rc;
+  fill_page_table(cfg, p.seq, block_table, page_size, num_pages, &p.pt);
+  p.indices = indices;
+  p.positions = positions;
+  p.status = static_cast<uint32_t*>(workspace);
+  const unsigned blocks = static_cast<unsigned>((p.total_rows + kPagedThreads - 1) / kPagedThreads);
+  launch_pdl(cache_positions_kernel, dim3(blocks), dim3(kPagedThreads), 0, static_cast<cudaStream_t>(stream), p);
+  return check_launch();
 }
 
 int pyramidkv_compress_layer_paged(const pkv_config* cfg, int32_t layer, pkv_tensor q_win, pkv_tensor k,

@@ -1,0 +1,514 @@
+// Pages of a growing cache: room for new rows, sequences that go on from others, and pages moved together.
+//
+// A page is free if no table entry names it (refs[page] == 0).  New pages are the lowest free ones in ascending order, dealt to
+// the requests in the order (layer, sequence, head, page), so the outcome depends on nothing but the inputs.  Three kernels:
+//   1. pages_carry_kernel   (`to` is another set of arrays, or sequences change places) tables, lens and refs of `to` from those
+//      of `from`, counts of shared pages adjusted.  Grid over the table, bound by its bytes.
+//   2. pages_deal_kernel / pages_pair_kernel   one cluster of 8 CTAs, because every page's place depends on all pages below it:
+//      each CTA sums its eighth of the requests and of refs, the eighths meet through distributed shared memory, and the free
+//      pages' ranks are found in a second pass over the eighths that are needed.  Bound by the latency of those passes; refs
+//      come from the L2 in 16-byte loads.
+//   3. pages_copy_kernel / pages_move_kernel   rows of part-filled pages to their copies, or whole pages downwards together with the
+//      tables that name them.  Bound by memory.
+// All or nothing: step 2 knows whether there is room before it changes anything; where step 1 has already written in place
+// (a fork), step 3 puts the staged tables back.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "pkv_common.cuh"
+
+namespace pkv {
+
+constexpr int kPgThreads = 1024;           // of a CTA of the cluster
+constexpr int kPgCluster = 8;
+constexpr int kPgCarryThreads = 256;
+constexpr int kPgCopyThreads = 128;
+
+// Tables, lens and refs of one side.
+struct PageArrays {
+  int32_t* tables;
+  int32_t* lens;
+  int32_t* refs;
+};
+
+struct PagesParams {
+  PageArrays from, to;                     // from: the staged copy where the call works in place and sequences change
+  PageArrays home;                         // from's own arrays (step 3 puts them back if there was no room)
+  PageArrays staged;                       // room for a copy of them in the workspace
+  void* k_pool;
+  void* v_pool;
+  int32_t* pos_pool;                       // or null
+  const int32_t* parents;                  // [to_batch], or null: everyone its own
+  const int32_t* add;                      // [layers][..], or null
+  int64_t add_stride;
+  int32_t* granted;                        // [layers][to_batch], or null
+  int32_t* used;                           // compaction, or null
+  int32_t layers, from_batch, to_batch, num_kv_heads, max_pages, page_size, num_pages;
+  int32_t carry;                           // step 1 runs
+  int32_t in_place;
+  int32_t row_pieces;                      // 16-byte pieces of a row
+  uint32_t* status;
+  int32_t* state;                          // [0] 1 if the call was met, [1] number of page moves
+  int32_t* list;                           // [num_pages] dealt pages; compaction: free pages to move into
+  int32_t* second;                         // [num_pages] compaction: pages that move
+  int32_t* place;                          // [num_pages] compaction: new place of every page from the border on
+  int32_t* unit_off;                       // [layers * to_batch] requests ahead of a sequence's
+};
+
+__device__ __forceinline__ int32_t pg_clamped(int32_t rows, const PagesParams& p) {
+  const int64_t most = static_cast<int64_t>(p.max_pages) * p.page_size;
+  return static_cast<int32_t>(min(static_cast<int64_t>(max(rows, 0)), most));
+}
+__device__ __forceinline__ int pg_pages(const PagesParams& p, int64_t rows) { return static_cast<int>((rows + p.page_size - 1) / p.page_size); }
+
+// What sequence c of `to` becomes in a layer.
+struct PgChild {
+  int parent;                              // -1: empty
+  bool first;                              // its parent's first child
+  int32_t rows, full, part;                // of the parent: rows, full pages, rows of the last page if it is not full
+  int32_t keeps;                           // pages whose entries it takes over
+  int64_t rows_new;
+  int pages;
+};
+__device__ __forceinline__ int pg_parent(const PagesParams& p, int c) {
+  if (!p.parents) return c;
+  const int par = __ldg(p.parents + c);
+  return par < 0 || par >= p.from_batch ? -1 : par;
+}
+__device__ __forceinline__ PgChild pg_child(const PagesParams& p, int l, int c, int parent, bool first) {
+  PgChild x;
+  x.parent = parent;
+  x.first = first;
+  x.rows = parent >= 0 ? pg_clamped(p.from.lens[static_cast<int64_t>(l) * p.from_batch + parent], p) : 0;
+  x.full = x.rows / p.page_size;
+  x.part = x.rows - x.full * p.page_size;
+  x.keeps = x.full + (x.part > 0 && first ? 1 : 0);
+  const int add = p.add ? max(__ldg(p.add + l * p.add_stride + c), 0) : 0;
+  x.rows_new = static_cast<int64_t>(x.rows) + add;
+  x.pages = static_cast<int>(min(static_cast<int64_t>(INT32_MAX), (x.rows_new + p.page_size - 1) / p.page_size));
+  return x;
+}
+
+// ------------------------------------------------------------------ staging of a call that works in place
+// grid-stride copy of from's own arrays to the staged ones.
+__global__ void __launch_bounds__(kPgCarryThreads) pages_stage_kernel(const __grid_constant__ PagesParams p) {
+  pdl_trigger();
+  pdl_wait();
+  const int64_t entries = static_cast<int64_t>(p.layers) * p.from_batch * p.num_kv_heads * p.max_pages;
+  const int64_t lens = static_cast<int64_t>(p.layers) * p.from_batch;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kPgCarryThreads + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * kPgCarryThreads;
+  for (int64_t i = at; i < entries; i += step) p.from.tables[i] = p.home.tables[i];
+  for (int64_t i = at; i < lens; i += step) p.from.lens[i] = p.home.lens[i];
+  for (int64_t i = at; i < p.num_pages; i += step) p.from.refs[i] = p.home.refs[i];
+}
+
+// refs of `to` from those of `from`: ahead of the next kernel where that one adjusts counts.
+__global__ void __launch_bounds__(kPgCarryThreads) pages_refs_kernel(const __grid_constant__ PagesParams p) {
+  pdl_trigger();
+  pdl_wait();
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kPgCarryThreads + threadIdx.x; i < p.num_pages; i += static_cast<int64_t>(gridDim.x) * kPgCarryThreads)
+    p.to.refs[i] = p.from.refs[i];
+}
+
+// ------------------------------------------------------------------ 1. what is carried over
+// grid (sequences of `to` and, where there are parents, of `from`; layers).  Entries that children keep are written to `to`;
+// a page gains a count for every child behind its first and loses one for a sequence without children.
+__global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __grid_constant__ PagesParams p) {
+  __shared__ int s_parent, s_first;
+  pdl_trigger();
+  pdl_wait();
+  const int l = blockIdx.y, c = blockIdx.x;
+  if (!p.parents && !p.in_place) {         // no count changes: they are copied on the way
+    const int64_t at = (static_cast<int64_t>(l) * gridDim.x + c) * kPgCarryThreads + threadIdx.x;
+    for (int64_t i = at; i < p.num_pages; i += static_cast<int64_t>(gridDim.x) * gridDim.y * kPgCarryThreads) p.to.refs[i] = p.from.refs[i];
+  }
+  if (c < p.to_batch) {
+    if (threadIdx.x == 0) {
+      s_parent = pg_parent(p, c);
+      s_first = 1;
+    }
+    __syncthreads();
+    const int parent = s_parent;
+    if (p.parents)
+      for (int i = threadIdx.x; i < c; i += kPgCarryThreads)
+        if (__ldg(p.parents + i) == parent) s_first = 0;
+    __syncthreads();
+    const PgChild x = pg_child(p, l, c, parent, s_first != 0);
+    if (parent < 0) return;
+    const int64_t src = (static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads * p.max_pages;
+    const int64_t dst = (static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads * p.max_pages;
+    const int64_t keeps = x.keeps, all = keeps * p.num_kv_heads;
+    for (int64_t i = threadIdx.x; i < all; i += kPgCarryThreads) {
+      const int64_t h = i / keeps, j = i - h * keeps;
+      const int entry = p.from.tables[src + h * p.max_pages + j];
+      p.to.tables[dst + h * p.max_pages + j] = entry;
+      if (!x.first && entry >= 0 && entry < p.num_pages) atomicAdd(p.to.refs + entry, 1);
+    }
+    return;
+  }
+  // a sequence of `from` that nobody goes on with: its pages are let go
+  const int b = c - p.to_batch;
+  if (threadIdx.x == 0) s_first = 1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.to_batch; i += kPgCarryThreads)
+    if (__ldg(p.parents + i) == b) s_first = 0;
+  __syncthreads();
+  if (!s_first) return;
+  const int rows = pg_clamped(p.from.lens[static_cast<int64_t>(l) * p.from_batch + b], p);
+  const int64_t pages = pg_pages(p, rows), all = pages * p.num_kv_heads;
+  const int64_t src = (static_cast<int64_t>(l) * p.from_batch + b) * p.num_kv_heads * p.max_pages;
+  for (int64_t i = threadIdx.x; i < all; i += kPgCarryThreads) {
+    const int64_t h = i / pages, j = i - h * pages;
+    const int entry = p.from.tables[src + h * p.max_pages + j];
+    if (entry >= 0 && entry < p.num_pages) atomicSub(p.to.refs + entry, 1);
+  }
+}
+
+// ------------------------------------------------------------------ 2. sums and ranks over a cluster
+struct PgShared {
+  int32_t warp[32];
+  int32_t block;                           // this CTA's sum, read by the others
+  int32_t flag;
+};
+
+// Exclusive running sum over the CTA's threads; *total: the CTA's sum.  Everybody takes part.
+__device__ __forceinline__ int pg_scan(PgShared& s, int x, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int run = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += y;
+  }
+  __syncthreads();                         // the last call's sums have been read
+  if (lane == 31) s.warp[warp] = run;
+  __syncthreads();
+  int w = s.warp[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += y;
+  }
+  *total = __shfl_sync(0xffffffffu, w, 31);
+  const int ahead = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+  return run - x + (warp ? ahead : 0);
+}
+
+// Sums of the CTAs of a cluster: what the CTAs ahead have, and all of them.
+__device__ __forceinline__ void pg_cluster(PgShared& s, int mine, int* ahead, int* total) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  if (threadIdx.x == 0) s.block = mine;
+  cluster.sync();
+  *ahead = *total = 0;
+  const int rank = static_cast<int>(cluster.block_rank());
+#pragma unroll
+  for (int c = 0; c < kPgCluster; ++c) {
+    const int x = *cluster.map_shared_rank(&s.block, c);
+    if (c < rank) *ahead += x;
+    *total += x;
+  }
+  cluster.sync();                          // everybody has read
+}
+
+// Four consecutive refs from `i` on (a multiple of four) as bits of free pages; pages behind `end` are not free.
+__device__ __forceinline__ uint32_t pg_free4(const int32_t* refs, bool aligned, int64_t i, int64_t end) {
+  uint32_t bits = 0;
+  if (aligned && i + 4 <= end) {
+    const int4 v = __ldcg(reinterpret_cast<const int4*>(refs + i));
+    bits = (v.x <= 0 ? 1u : 0u) | (v.y <= 0 ? 2u : 0u) | (v.z <= 0 ? 4u : 0u) | (v.w <= 0 ? 8u : 0u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < end && __ldcg(refs + i + e) <= 0) bits |= 1u << e;
+  }
+  return bits;
+}
+
+// This CTA's eighth of 0 .. n - 1, its borders multiples of four.
+__device__ __forceinline__ void pg_share(int64_t n, int rank, int64_t* lo, int64_t* hi) {
+  const int64_t per = ((n + kPgCluster - 1) / kPgCluster + 3) / 4 * 4;
+  *lo = min(n, per * rank);
+  *hi = min(n, per * (rank + 1));
+}
+
+// Free pages among lo .. hi - 1, counted by the CTA.
+__device__ __forceinline__ int pg_count_free(PgShared& s, const int32_t* refs, int64_t lo, int64_t hi) {
+  const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
+  int free = 0, total;
+  for (int64_t i = lo + threadIdx.x * 4; i < hi; i += kPgThreads * 4) free += __popc(pg_free4(refs, aligned, i, hi));
+  pg_scan(s, free, &total);
+  return total;
+}
+
+// Calls take(page, rank) for the free pages among lo .. hi - 1 whose rank (from `ahead` on) is below `need`.
+template <typename F>
+__device__ __forceinline__ void pg_rank_free(PgShared& s, const int32_t* refs, int64_t lo, int64_t hi, int ahead, int need, F&& take) {
+  const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
+  for (int64_t base = lo; base < hi && ahead < need; base += kPgThreads * 4) {     // (uniform over the CTA)
+    const int64_t i = base + threadIdx.x * 4;
+    const uint32_t bits = i < hi ? pg_free4(refs, aligned, i, hi) : 0u;
+    int total;
+    int rank = ahead + pg_scan(s, __popc(bits), &total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if ((bits >> e) & 1u) {
+        if (rank < need) take(static_cast<int32_t>(i + e), rank);
+        ++rank;
+      }
+    ahead += total;
+  }
+}
+
+// One cluster.  Requests are counted, free pages found and dealt out; lens, granted and the new table entries of `to` are written.
+__global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_constant__ PagesParams p) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  __shared__ PgShared s;
+  __shared__ int32_t s_parent[PKV_MAX_CACHE_BATCH];              // bit 30: not the parent's first child
+  __shared__ int32_t s_child[PKV_MAX_CACHE_BATCH];               // a parent's first child
+  pdl_trigger();
+  const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
+  pdl_wait();
+  if (tid == 0) s.flag = 0;
+  for (int b = tid; b < p.from_batch; b += kPgThreads) s_child[b] = INT32_MAX;
+  __syncthreads();
+  int bad = 0;                             // bit 0: a parent outside the batch, bit 1: a sequence too long for its table
+  for (int c = tid; c < p.to_batch; c += kPgThreads) {
+    const int parent = pg_parent(p, c);
+    if (p.parents && parent < 0 && __ldg(p.parents + c) != -1) bad |= 1;
+    if (parent >= 0) atomicMin(&s_child[parent], c);
+    s_parent[c] = parent;
+  }
+  __syncthreads();
+  for (int c = tid; c < p.to_batch; c += kPgThreads)
+    if (s_parent[c] >= 0 && s_child[s_parent[c]] != c) s_parent[c] |= 1 << 30;
+  __syncthreads();
+  const int64_t units = static_cast<int64_t>(p.layers) * p.to_batch;
+  int64_t lo, hi;
+  pg_share(units, rank, &lo, &hi);
+  auto child = [&](int64_t unit) {
+    const int l = static_cast<int>(unit / p.to_batch), c = static_cast<int>(unit - static_cast<int64_t>(l) * p.to_batch);
+    const int x = s_parent[c];
+    return pg_child(p, l, c, x < 0 ? -1 : x & ~(1 << 30), x >= 0 && !(x >> 30));
+  };
+  // requests of every unit; each thread has consecutive ones
+  const int64_t per = (hi - lo + kPgThreads - 1) / kPgThreads, u0 = min(hi, lo + per * tid), u1 = min(hi, u0 + per);
+  int64_t mine = 0;
+  for (int64_t u = u0; u < u1; ++u) {
+    const PgChild x = child(u);
+    if (x.pages > p.max_pages) bad |= 2;
+    else mine += static_cast<int64_t>(x.pages - x.keeps) * p.num_kv_heads;
+  }
+  // more requests than pages cannot be met; sums stay within 32 bits that way
+  if (mine > p.num_pages) { bad |= 2; mine = 0; }
+  if (bad) atomicOr(&s.flag, bad);
+  int sum, ahead, need;
+  // (1024 threads x num_pages may pass 32 bits: the sum is formed in halves)
+  int sum_high;
+  const int my_low = static_cast<int>(mine & 0xffff), my_high = static_cast<int>(mine >> 16);
+  const int run_low = pg_scan(s, my_low, &sum), run_high = pg_scan(s, my_high, &sum_high);
+  const int64_t cta = static_cast<int64_t>(sum) + (static_cast<int64_t>(sum_high) << 16);
+  const bool too_many = cta > p.num_pages;
+  if (too_many && tid == 0) s.flag |= 2;
+  __syncthreads();
+  pg_cluster(s, too_many ? 0 : static_cast<int>(cta), &ahead, &need);
+  int flags = 0;
+#pragma unroll
+  for (int c = 0; c < kPgCluster; ++c) flags |= *cluster.map_shared_rank(&s.flag, c);
+  int64_t flo, fhi;
+  pg_share(p.num_pages, rank, &flo, &fhi);
+  const int free_here = pg_count_free(s, p.to.refs, flo, fhi);
+  int free_ahead, free_all;
+  pg_cluster(s, free_here, &free_ahead, &free_all);
+  const bool met = flags == 0 && static_cast<uint32_t>(need) <= static_cast<uint32_t>(free_all);
+  if (rank == 0 && tid == 0) {
+    p.state[0] = met ? 1 : 0;
+    if (!met) atomicOr(p.status, (flags & 1 ? kStatusBadIndex : 0u) | ((flags & 2) || flags == 0 ? kStatusNoRoom : 0u));
+  }
+  if (!met) {                              // the same in the whole cluster
+    if (p.granted)
+      for (int64_t u = u0; u < u1; ++u) p.granted[u] = 0;
+    return;
+  }
+  pg_rank_free(s, p.to.refs, flo, fhi, free_ahead, need, [&](int32_t page, int r) {
+    p.list[r] = page;
+    p.to.refs[page] = 1;
+  });
+  int64_t off = ahead + static_cast<int64_t>(run_low) + (static_cast<int64_t>(run_high) << 16);
+  for (int64_t u = u0; u < u1; ++u) {
+    const PgChild x = child(u);
+    p.unit_off[u] = static_cast<int32_t>(off);
+    off += static_cast<int64_t>(x.pages - x.keeps) * p.num_kv_heads;
+  }
+  cluster.sync();                          // list and offsets are there (and so are everybody's reads of lens)
+  // table entries: a warp per head of a unit
+  const int lane = tid & 31;
+  const int64_t heads = units * p.num_kv_heads;
+  for (int64_t i = static_cast<int64_t>(rank) * (kPgThreads / 32) + (tid >> 5); i < heads; i += kPgCluster * (kPgThreads / 32)) {
+    const int64_t u = i / p.num_kv_heads;
+    const int h = static_cast<int>(i - u * p.num_kv_heads);
+    const PgChild x = child(u);
+    const int fresh = x.pages - x.keeps;
+    if (!fresh) continue;
+    const int32_t* pages = p.list + __ldcg(p.unit_off + u) + static_cast<int64_t>(h) * fresh;
+    int32_t* table = p.to.tables + (u * p.num_kv_heads + h) * p.max_pages + x.keeps;
+    for (int j = lane; j < fresh; j += 32) table[j] = __ldcg(pages + j);
+  }
+  cluster.sync();                          // lens of `from` may be those of `to`: they change behind everybody's last look
+  for (int64_t u = u0; u < u1; ++u) {
+    const PgChild x = child(u);
+    p.to.lens[u] = static_cast<int32_t>(x.rows_new);
+    if (p.granted) p.granted[u] = static_cast<int32_t>(x.rows_new - x.rows);
+  }
+}
+
+// ------------------------------------------------------------------ 3. rows of a part-filled page to its copies
+// grid (sequences of `to`, layers, heads).  If the call was not met: puts `to` back (in place), a share per CTA.
+__global__ void __launch_bounds__(kPgCopyThreads) pages_copy_kernel(const __grid_constant__ PagesParams p) {
+  __shared__ int s_first;
+  pdl_trigger();
+  pdl_wait();
+  const int c = blockIdx.x, l = blockIdx.y, h = blockIdx.z;
+  if (!p.state[0]) {
+    if (!p.in_place) return;
+    const int64_t cta = (static_cast<int64_t>(h) * gridDim.y + l) * gridDim.x + c, ctas = static_cast<int64_t>(gridDim.x) * gridDim.y * gridDim.z;
+    const int64_t at = cta * kPgCopyThreads + threadIdx.x, step = ctas * kPgCopyThreads;
+    const int64_t entries = static_cast<int64_t>(p.layers) * p.from_batch * p.num_kv_heads * p.max_pages;
+    for (int64_t i = at; i < entries; i += step) p.home.tables[i] = p.from.tables[i];
+    for (int64_t i = at; i < p.num_pages; i += step) p.home.refs[i] = p.from.refs[i];
+    return;                                // lens were not written
+  }
+  const int parent = pg_parent(p, c);
+  if (parent < 0) return;
+  if (threadIdx.x == 0) s_first = 1;
+  __syncthreads();
+  for (int i = threadIdx.x; i < c; i += kPgCopyThreads)
+    if (__ldg(p.parents + i) == parent) s_first = 0;
+  __syncthreads();
+  const PgChild x = pg_child(p, l, c, parent, s_first != 0);
+  if (x.first || !x.part) return;
+  const int src = p.from.tables[((static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads + h) * p.max_pages + x.full];
+  const int dst = p.to.tables[((static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads + h) * p.max_pages + x.full];
+  if (src < 0 || src >= p.num_pages) {
+    if (threadIdx.x == 0) atomicOr(p.status, kStatusBadPage);
+    return;
+  }
+  const int64_t page = static_cast<int64_t>(p.page_size) * p.row_pieces;
+  const uint4* ks = static_cast<const uint4*>(p.k_pool) + src * page;
+  const uint4* vs = static_cast<const uint4*>(p.v_pool) + src * page;
+  uint4* kd = static_cast<uint4*>(p.k_pool) + dst * page;
+  uint4* vd = static_cast<uint4*>(p.v_pool) + dst * page;
+  const int64_t pieces = static_cast<int64_t>(x.part) * p.row_pieces;
+  for (int64_t i = threadIdx.x; i < pieces; i += kPgCopyThreads) {
+    const uint4 a = ks[i], b = vs[i];
+    kd[i] = a;
+    vd[i] = b;
+  }
+  if (p.pos_pool)
+    for (int i = threadIdx.x; i < x.part; i += kPgCopyThreads)
+      p.pos_pool[static_cast<int64_t>(dst) * p.page_size + i] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + i];
+}
+
+// ------------------------------------------------------------------ compaction
+// One cluster.  With u pages in use, the free pages below u (list) and the used ones from u on (second) are as many; the i-th
+// of the latter moves to the i-th of the former.
+__global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_constant__ PagesParams p) {
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  __shared__ PgShared s;
+  pdl_trigger();
+  const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
+  pdl_wait();
+  int64_t lo, hi;
+  pg_share(p.num_pages, rank, &lo, &hi);
+  const int free_here = pg_count_free(s, p.from.refs, lo, hi);
+  int free_ahead, free_all;
+  pg_cluster(s, free_here, &free_ahead, &free_all);
+  const int used = p.num_pages - free_all;
+  // free pages below `used`, in this CTA's share and the ones ahead of it
+  const int64_t cut = min(max(static_cast<int64_t>(used), lo), hi);
+  const int holes_here = pg_count_free(s, p.from.refs, lo, cut);
+  int holes_ahead, moves;
+  pg_cluster(s, holes_here, &holes_ahead, &moves);
+  if (rank == 0 && tid == 0) {
+    p.state[0] = used;
+    p.state[1] = moves;
+    if (p.used) *p.used = used;
+  }
+  pg_rank_free(s, p.from.refs, lo, cut, holes_ahead, moves, [&](int32_t page, int r) { p.list[r] = page; });
+  // used pages from `used` on: their rank is their distance from `used` less the free ones between
+  const int movers_here = static_cast<int>(hi - cut) - (free_here - holes_here);
+  int movers_ahead, movers;
+  pg_cluster(s, movers_here, &movers_ahead, &movers);
+  const bool aligned = reinterpret_cast<uintptr_t>(p.from.refs) % 16 == 0;
+  int ahead = movers_ahead;
+  for (int64_t base = cut / 4 * 4; base < hi; base += kPgThreads * 4) {            // (uniform over the CTA)
+    const int64_t i = base + tid * 4;
+    uint32_t there = 0, bits = 0;
+    if (i < hi) {
+      there = (i + 4 <= hi ? 15u : (1u << (hi - i)) - 1u) & ~(i < cut ? (1u << (cut - i)) - 1u : 0u);
+      bits = there & ~pg_free4(p.from.refs, aligned, i, hi);
+    }
+    int total;
+    int r = ahead + pg_scan(s, __popc(bits), &total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((bits >> e) & 1u) p.second[r++] = static_cast<int32_t>(i + e);
+      else if ((there >> e) & 1u) p.place[i + e] = static_cast<int32_t>(i + e);    // free: nothing should name it
+    }
+    ahead += total;
+  }
+  cluster.sync();                          // both lists are there
+  for (int m = rank * kPgThreads + tid; m < moves; m += kPgCluster * kPgThreads) p.place[__ldcg(p.second + m)] = __ldcg(p.list + m);
+}
+
+// Three independent jobs, each dealt out over the grid: pages to their new places, tables with the new places, refs of `to`.
+__global__ void __launch_bounds__(kPgCopyThreads) pages_move_kernel(const __grid_constant__ PagesParams p) {
+  pdl_trigger();
+  pdl_wait();
+  const int used = p.state[0], moves = p.state[1];
+  const int64_t page = static_cast<int64_t>(p.page_size) * p.row_pieces;
+  for (int m = blockIdx.x; m < moves; m += gridDim.x) {
+    const int dst = p.list[m], src = p.second[m];
+    const uint4* ks = static_cast<const uint4*>(p.k_pool) + src * page;
+    const uint4* vs = static_cast<const uint4*>(p.v_pool) + src * page;
+    uint4* kd = static_cast<uint4*>(p.k_pool) + dst * page;
+    uint4* vd = static_cast<uint4*>(p.v_pool) + dst * page;
+    for (int64_t i = threadIdx.x; i < page; i += kPgCopyThreads) {
+      const uint4 a = ks[i], b = vs[i];
+      kd[i] = a;
+      vd[i] = b;
+    }
+    if (p.pos_pool)
+      for (int i = threadIdx.x; i < p.page_size; i += kPgCopyThreads)
+        p.pos_pool[static_cast<int64_t>(dst) * p.page_size + i] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + i];
+  }
+  const int64_t units = static_cast<int64_t>(p.layers) * p.from_batch;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int rows = p.from.lens[unit];
+    const int pages = pg_pages(p, pg_clamped(rows, p));
+    const int64_t at = unit * p.num_kv_heads * p.max_pages, all = static_cast<int64_t>(pages) * p.num_kv_heads;
+    for (int64_t i = threadIdx.x; i < all; i += kPgCopyThreads) {
+      const int64_t h = i / pages, e = at + h * p.max_pages + (i - h * pages);
+      const int entry = p.from.tables[e];
+      const int place = entry >= used && entry < p.num_pages ? p.place[entry] : entry;
+      if (!p.in_place || place != entry) p.to.tables[e] = place;
+    }
+    if (!p.in_place && threadIdx.x == 0) p.to.lens[unit] = rows;
+  }
+  // A free page below the border has its new tenant's count, a page from the border on none.
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kPgCopyThreads + threadIdx.x, step = static_cast<int64_t>(gridDim.x) * kPgCopyThreads;
+  if (!p.in_place)
+    for (int64_t i = at; i < p.num_pages; i += step) {
+      const int count = i < used ? p.from.refs[i] : 0;
+      if (i >= used || count > 0) p.to.refs[i] = count;
+    }
+  for (int64_t m = at; m < moves; m += step) {
+    p.to.refs[p.list[m]] = p.from.refs[p.second[m]];
+    if (p.in_place) p.to.refs[p.second[m]] = 0;
+  }
+}
+
+}  // namespace pkv

@@ -36,6 +36,7 @@ enum : uint32_t {
   kStatusWaitExpired = 1u << 1,      // a bounded wait ran out
   kStatusBadPage = 1u << 2,          // a block-table entry named a page outside the pool (row skipped)
   kStatusBadIndex = 1u << 3,         // a caller-supplied index list named a position outside its sequence (row skipped)
+  kStatusNoRoom = 1u << 4,           // a page call found too few free pages, or a sequence longer than its table (nothing changed)
 };
 
 // Programmatic dependent launch: every kernel of the library is launched so that it may start while

@@ -24,6 +24,7 @@
 #include <cooperative_groups.h>
 
 #include "pkv_common.cuh"
+#include "pkv_mma16.cuh"
 #include "pkv_paged.cuh"
 
 namespace pkv {
@@ -346,39 +347,6 @@ __global__ void __launch_bounds__(kDecThreads) decode_attention_kernel(const Dec
 // ------------------------------------------------------------------ 16-bit rows
 constexpr int kDecMmaHeads = 4;           // query heads per CTA: 4 heads x 3 parts of the weights in the 16 rows of an MMA
 
-template <typename T>
-struct Dec16;
-template <>
-struct Dec16<__nv_bfloat16> {
-  static constexpr float kShift = 0.f;    // bfloat16 has the range of fp32
-  __device__ __forceinline__ static uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  __device__ __forceinline__ static float2 unpack(uint32_t u) {
-    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
-  }
-  __device__ __forceinline__ static void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-};
-template <>
-struct Dec16<__half> {
-  static constexpr float kShift = 13.f;   // weights carry 2^13, so that the third part of small ones is not subnormal
-  __device__ __forceinline__ static uint32_t pack(float lo, float hi) {
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  __device__ __forceinline__ static float2 unpack(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
-  __device__ __forceinline__ static void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-};
-
 // One head's sums over a warp's rows on the fp32 pipe, D / 32 channels per lane: for rows that hold infinities or NaN.  In the
 // matrix product every part of a weight meets every value, and a part that is zero or negative makes NaN of an infinity;
 // one weight, one product gives what the sum says (an infinity of the value's sign, NaN where both signs or NaN are
@@ -413,16 +381,6 @@ __device__ __forceinline__ void dec_sum_special(const DecodeParams& p, int b, in
     }
 #pragma unroll
   for (int c = 0; c < PER; ++c) acc[lane * PER + c] = a[c];
-}
-
-// Bytes from global to shared memory past the registers, zeros where `there` is false.
-__device__ __forceinline__ void dec_copy16(uint32_t to, const void* from, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16u : 0u) : "memory");
-}
-__device__ __forceinline__ uint4 dec_lds16(uint32_t at) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
 }
 
 // grid, cluster as above, WARPS warps, kDecMmaHeads query heads per CTA.  A warp takes tiles of 16 rows, STAGES of them in

@@ -76,4 +76,30 @@ __global__ void __launch_bounds__(kPagedThreads) gather_paged_kernel(const Gathe
   static_cast<uint4*>(p.v_pool)[dst] = reinterpret_cast<const uint4*>(vsrc)[piece];
 }
 
+struct CachePositionsParams {
+  const int32_t* indices;   // packed rows: original position of each kept row
+  int32_t* positions;       // [num_pages][page_size]
+  SeqTable seq;
+  PageTable pt;
+  int64_t total_rows;
+  uint32_t* status;
+};
+
+// One thread moves one kept row's position to the row's slot.
+__global__ void __launch_bounds__(kPagedThreads) cache_positions_kernel(const __grid_constant__ CachePositionsParams p) {
+  pdl_trigger();
+  pdl_wait();
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kPagedThreads + threadIdx.x;
+  if (row >= p.total_rows) return;
+  int b = 0;
+  while (b + 1 < p.seq.batch && row >= p.seq.row_off[b + 1]) ++b;
+  const int64_t local = row - p.seq.row_off[b];
+  const int h = static_cast<int>(local / p.seq.count[b]);
+  const int64_t slot = paged_row(p.pt, b, h, static_cast<int>(local - static_cast<int64_t>(h) * p.seq.count[b]));
+  const int pos = p.indices[row];
+  if (slot < 0) atomicOr(p.status, kStatusBadPage);
+  else if (pos < 0 || pos >= p.seq.n[b]) atomicOr(p.status, kStatusBadIndex);
+  else p.positions[slot] = pos;
+}
+
 }  // namespace pkv

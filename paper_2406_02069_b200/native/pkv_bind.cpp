@@ -18,6 +18,7 @@
 #include <vector>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -325,6 +326,219 @@ PyObject* decode_attention_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------- growing cache
+PyObject* g_cache_type = nullptr;        // cache.PkvCache, cache.PkvRotary
+PyObject* g_rotary_type = nullptr;
+
+// cache.PkvCache: the struct that the library takes, and behind it what it was made for.
+struct CacheObject {
+  pkv_cache cache;
+  int32_t heads_kv, head_dim, dtype, device;
+};
+
+// A ctypes structure of a known type, read through its buffer.
+struct Struct {
+  Py_buffer buf{};
+  ~Struct() { if (buf.obj) PyBuffer_Release(&buf); }
+  const void* open(PyObject* o, PyObject* type, size_t size) {
+    if (!type || PyObject_IsInstance(o, type) != 1 || PyObject_GetBuffer(o, &buf, PyBUF_SIMPLE) != 0) { PyErr_Clear(); return nullptr; }
+    return buf.len == static_cast<Py_ssize_t>(size) ? buf.buf : nullptr;
+  }
+};
+
+// What every call on a cache starts with.  A call without one (rotary) has the device of its tensors instead.
+struct CacheCall {
+  Struct cfg_buf, cache_buf, plan_buf;
+  const pkv_config* cfg = nullptr;
+  const CacheObject* of = nullptr;
+  const pkv_rotary* plan = nullptr;
+  int device = -1;
+  void* stream = nullptr;
+
+  bool open_config(PyObject* o) {
+    cfg = static_cast<const pkv_config*>(cfg_buf.open(o, g_config_type, sizeof(pkv_config)));
+    if (!cfg || cfg->num_kv_heads < 1 || cfg->dtype < PKV_DTYPE_FP32 || cfg->dtype > PKV_DTYPE_FP16) return false;
+    device = c10::cuda::current_device();
+    return true;
+  }
+  bool open_cache(PyObject* o, Struct* at, const CacheObject** out) const {
+    *out = static_cast<const CacheObject*>(at->open(o, g_cache_type, sizeof(CacheObject)));
+    return *out && (*out)->heads_kv == cfg->num_kv_heads && (*out)->head_dim == cfg->head_dim && (*out)->dtype == cfg->dtype && (*out)->device == device;
+  }
+  bool open(PyObject* config, PyObject* cache) { return open_config(config) && open_cache(cache, &cache_buf, &of); }
+  bool open_plan(PyObject* o) {
+    plan = static_cast<const pkv_rotary*>(plan_buf.open(o, g_rotary_type, sizeof(pkv_rotary)));
+    return plan != nullptr;
+  }
+  bool on_stream(PyObject* stream_or_none) {
+    if (stream_or_none == Py_None) {
+      stream = c10::cuda::getCurrentCUDAStream().stream();
+      return true;
+    }
+    PyObject* s = PyObject_GetAttrString(stream_or_none, "cuda_stream");
+    if (!s) { PyErr_Clear(); return false; }
+    stream = PyLong_AsVoidPtr(s);
+    Py_DECREF(s);
+    if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+    return true;
+  }
+  bool here(PyObject* o, View* v) const { return get(o, v) && v->t->get_device() == device; }
+  // [batch][heads][tokens][d] rows of the configured type
+  bool rows(PyObject* o, View* v, int64_t batch, int64_t heads, int64_t tokens) const {
+    return here(o, v) && v->t->dim() == 4 && v->t->scalar_type() == scalar_type(cfg) && v->size(0) == batch && v->size(1) == heads &&
+           v->size(2) == tokens && v->size(3) == cfg->head_dim && v->stride(3) == 1;
+  }
+  // A dimension of one entry has no say in where rows lie.
+  pkv_tensor strided(const View& v) const {
+    if (!v) return pkv_tensor{nullptr, 0, 0, 0};
+    const int64_t d = cfg->head_dim;
+    return pkv_tensor{v.ptr(), v.size(0) > 1 ? v.stride(0) : d, v.size(1) > 1 ? v.stride(1) : d, v.size(2) > 1 ? v.stride(2) : d};
+  }
+  bool positions(PyObject* o, View* v, int64_t batch, int64_t tokens, int64_t* stride) const {
+    if (!here(o, v) || v->t->dim() != 2 || v->t->scalar_type() != c10::kInt || v->size(0) != batch || v->size(1) != tokens ||
+        (tokens > 1 && v->stride(1) != 1))
+      return false;
+    *stride = batch > 1 ? v->stride(0) : 0;
+    return true;
+  }
+  // A contiguous tensor of a type and shape (-1: dimension not there).
+  bool shaped(PyObject* o, View* v, c10::ScalarType type, int64_t n0, int64_t n1 = -1, int64_t n2 = -1) const {
+    const int dims = n1 < 0 ? 1 : (n2 < 0 ? 2 : 3);
+    return here(o, v) && v->t->dim() == dims && v->t->scalar_type() == type && v->size(0) == n0 && (n1 < 0 || v->size(1) == n1) &&
+           (n2 < 0 || v->size(2) == n2) && v->t->is_contiguous();
+  }
+  bool workspace(PyObject* o, View* v) const { return here(o, v) && v->t->scalar_type() == c10::kByte && v->t->is_contiguous(); }
+  bool add(PyObject* o, View* v, int64_t batch, int64_t* stride) const {
+    if (!here(o, v) || v->t->scalar_type() != c10::kInt) return false;
+    const int64_t layers = of->cache.layers, last = v->t->dim() - 1;
+    if (last == 0 ? v->size(0) != batch : (last != 1 || v->size(0) != layers || v->size(1) != batch)) return false;
+    if (batch > 1 && v->stride(static_cast<int>(last)) != 1) return false;
+    *stride = last == 1 && layers > 1 ? v->stride(0) : 0;
+    return true;
+  }
+};
+
+bool as_float(PyObject* o, float* out) {
+  const double v = PyFloat_Check(o) ? PyFloat_AS_DOUBLE(o) : (PyLong_Check(o) ? PyLong_AsDouble(o) : -1.0);
+  if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+  *out = static_cast<float>(v);
+  return PyFloat_Check(o) || PyLong_Check(o);
+}
+int32_t* ints(const View& v) { return v ? static_cast<int32_t*>(v.ptr()) : nullptr; }
+float* floats(const View& v) { return v ? static_cast<float*>(v.ptr()) : nullptr; }
+size_t bytes_of(const View& ws) { return static_cast<size_t>(ws.t->numel()); }
+
+// (cfg, plan, positions, q, k, q_out, k_out, inverse, stream); q or k and its output may be None
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  View pos, q, k, qo, ko;
+  int64_t stride;
+  if (n != 9 || !c.open_config(a[0]) || !c.open_plan(a[1])) return not_taken();
+  PyObject* some = a[3] != Py_None ? a[3] : a[4];
+  View first;
+  if (!c.here(some, &first) || first.t->dim() != 4) return not_taken();
+  const int64_t batch = first.size(0), tokens = first.size(2);
+  if (batch < 1 || tokens < 1 || batch * tokens > INT32_MAX || !c.positions(a[2], &pos, batch, tokens, &stride)) return not_taken();
+  if (a[3] != Py_None && (!c.rows(a[3], &q, batch, c.cfg->num_q_heads, tokens) || !c.rows(a[5], &qo, batch, c.cfg->num_q_heads, tokens))) return not_taken();
+  if (a[4] != Py_None && (!c.rows(a[4], &k, batch, c.cfg->num_kv_heads, tokens) || !c.rows(a[6], &ko, batch, c.cfg->num_kv_heads, tokens))) return not_taken();
+  if (!c.on_stream(a[8])) return not_taken();
+  const int inverse = PyObject_IsTrue(a[7]);
+  return without_gil([&] {
+    return pyramidkv_rotary(c.cfg, c.plan, ints(pos), stride, static_cast<int32_t>(batch), static_cast<int32_t>(tokens), c.strided(q), c.strided(qo),
+                            c.strided(k), c.strided(ko), inverse, c.stream);
+  });
+}
+
+// (cfg, cache, layer, positions, k, v, workspace, q, q_out, plan, counts, stream)
+PyObject* append_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  View pos, q, qo, k, v, counts, ws;
+  int32_t layer;
+  int64_t stride = 0;
+  if (n != 12 || !as_int32(a[2], &layer) || !c.open(a[0], a[1]) || !c.here(a[4], &k) || k.t->dim() != 4) return not_taken();
+  const int64_t batch = c.of->cache.batch, tokens = k.size(2);
+  if (tokens < 1 || tokens > INT32_MAX || !c.rows(a[4], &k, batch, c.cfg->num_kv_heads, tokens) || !c.rows(a[5], &v, batch, c.cfg->num_kv_heads, tokens) ||
+      !c.workspace(a[6], &ws) || (a[9] != Py_None && !c.open_plan(a[9])) ||
+      (a[3] == Py_None ? c.plan || c.of->cache.positions : !c.positions(a[3], &pos, batch, tokens, &stride)) ||
+      (a[10] != Py_None && !c.shaped(a[10], &counts, c10::kInt, batch)))
+    return not_taken();
+  if (a[7] != Py_None && (!c.rows(a[7], &q, batch, c.cfg->num_q_heads, tokens) || !c.rows(a[8], &qo, batch, c.cfg->num_q_heads, tokens))) return not_taken();
+  if (!c.on_stream(a[11])) return not_taken();
+  return without_gil([&] {
+    return pyramidkv_append_cache(c.cfg, &c.of->cache, layer, c.plan, ints(pos), stride, static_cast<int32_t>(tokens), c.strided(q), c.strided(qo),
+                                  c.strided(k), c.strided(v), ints(counts), ws.ptr(), bytes_of(ws), c.stream);
+  });
+}
+
+// (cfg, cache, layer, q, out, workspace, q_positions, lse, scale, softcap, slopes, window, prefix, stream)
+PyObject* decode_attention_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  View q, out, ws, pos, lse, slopes;
+  int32_t layer;
+  pkv_attend_options o{};
+  if (n != 14 || !as_int32(a[2], &layer) || !c.open(a[0], a[1]) || !as_float(a[8], &o.scale) || !as_float(a[9], &o.softcap) ||
+      !as_int32(a[11], &o.window) || !as_int32(a[12], &o.prefix))
+    return not_taken();
+  const int64_t batch = c.of->cache.batch, heads = c.cfg->num_q_heads, d = c.cfg->head_dim;
+  if (!c.here(a[3], &q) || q.t->scalar_type() != scalar_type(c.cfg)) return not_taken();
+  const int last = static_cast<int>(q.t->dim()) - 1;              // [batch][H_q][d] or [batch][H_q][1][d]
+  if ((last != 2 && (last != 3 || q.size(2) != 1)) || q.size(0) != batch || q.size(1) != heads || q.size(last) != d || q.stride(last) != 1 ||
+      !c.shaped(a[4], &out, c10::kFloat, batch, heads, d) || !c.workspace(a[5], &ws) || (a[6] != Py_None && !c.shaped(a[6], &pos, c10::kInt, batch)) ||
+      (a[7] != Py_None && !c.shaped(a[7], &lse, c10::kFloat, batch, heads)) || (a[10] != Py_None && !c.shaped(a[10], &slopes, c10::kFloat, heads)) ||
+      !c.on_stream(a[13]))
+    return not_taken();
+  o.slopes = floats(slopes);
+  o.q_positions = ints(pos);
+  const pkv_tensor view{q.ptr(), batch > 1 ? q.stride(0) : 0, heads > 1 ? q.stride(1) : 0, 0};
+  return without_gil([&] {
+    return pyramidkv_decode_attention_cache(c.cfg, &c.of->cache, layer, &o, view, floats(out), floats(lse), ws.ptr(), bytes_of(ws), c.stream);
+  });
+}
+
+// (cfg, cache, to, add, granted, workspace, stream)
+PyObject* cache_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  Struct to_buf;
+  const CacheObject* to;
+  View add, granted, ws;
+  int64_t stride;
+  if (n != 7 || !c.open(a[0], a[1]) || !c.open_cache(a[2], &to_buf, &to) || !c.of->cache.refs || !to->cache.refs ||
+      !c.add(a[3], &add, c.of->cache.batch, &stride) || (a[4] != Py_None && !c.shaped(a[4], &granted, c10::kInt, c.of->cache.layers, to->cache.batch)) ||
+      !c.workspace(a[5], &ws) || !c.on_stream(a[6]))
+    return not_taken();
+  return without_gil([&] {
+    return pyramidkv_cache_reserve(c.cfg, &c.of->cache, &to->cache, ints(add), stride, ints(granted), ws.ptr(), bytes_of(ws), c.stream);
+  });
+}
+
+// (cfg, cache, to, parents, add, granted, workspace, stream)
+PyObject* cache_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  Struct to_buf;
+  const CacheObject* to;
+  View parents, add, granted, ws;
+  int64_t stride = 0;
+  if (n != 8 || !c.open(a[0], a[1]) || !c.open_cache(a[2], &to_buf, &to) || !c.of->cache.refs || !to->cache.refs ||
+      !c.shaped(a[3], &parents, c10::kInt, to->cache.batch) || (a[4] != Py_None && !c.add(a[4], &add, to->cache.batch, &stride)) ||
+      (a[5] != Py_None && !c.shaped(a[5], &granted, c10::kInt, c.of->cache.layers, to->cache.batch)) || !c.workspace(a[6], &ws) || !c.on_stream(a[7]))
+    return not_taken();
+  return without_gil([&] {
+    return pyramidkv_cache_fork(c.cfg, &c.of->cache, &to->cache, ints(parents), ints(add), stride, ints(granted), ws.ptr(), bytes_of(ws), c.stream);
+  });
+}
+
+// (cfg, cache, to, used, workspace, stream)
+PyObject* cache_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CacheCall c;
+  Struct to_buf;
+  const CacheObject* to;
+  View used, ws;
+  if (n != 6 || !c.open(a[0], a[1]) || !c.open_cache(a[2], &to_buf, &to) || !c.of->cache.refs || !to->cache.refs ||
+      (a[3] != Py_None && !c.shaped(a[3], &used, c10::kInt, 1)) || !c.workspace(a[4], &ws) || !c.on_stream(a[5]))
+    return not_taken();
+  return without_gil([&] { return pyramidkv_cache_compact(c.cfg, &c.of->cache, &to->cache, ints(used), ws.ptr(), bytes_of(ws), c.stream); });
+}
+
 // A tensor that cannot be asked for its data (a fake one, say) or a CUDA runtime that does not answer throws: left to the
 // other path too.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
@@ -345,10 +559,25 @@ PyObject* set_config_type(PyObject*, PyObject* type) {
   Py_RETURN_NONE;
 }
 
+// (cache type, plan type): the classes of the growing cache's structures.
+PyObject* set_cache_types(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 2) { PyErr_SetString(PyExc_TypeError, "set_cache_types takes two classes"); return nullptr; }
+  PyObject** to[2] = {&g_cache_type, &g_rotary_type};
+  for (int i = 0; i < 2; ++i) {
+    Py_INCREF(a[i]);
+    Py_XDECREF(*to[i]);
+    *to[i] = a[i];
+  }
+  Py_RETURN_NONE;
+}
+
 #define PKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PKV_METHOD(compress_layer), PKV_METHOD(attend_compress_layer), PKV_METHOD(compress_layer_paged),
                          PKV_METHOD(score_window), PKV_METHOD(select_topk), PKV_METHOD(gather_compact), PKV_METHOD(decode_attention),
-                         PKV_METHOD(decode_attention_paged), {"set_config_type", set_config_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         PKV_METHOD(decode_attention_paged), PKV_METHOD(rotary), PKV_METHOD(append_cache), PKV_METHOD(decode_attention_cache),
+                         PKV_METHOD(cache_reserve), PKV_METHOD(cache_fork), PKV_METHOD(cache_compact),
+                         {"set_cache_types", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(set_cache_types)), METH_FASTCALL, nullptr},
+                         {"set_config_type", set_config_type, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_pkv_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
