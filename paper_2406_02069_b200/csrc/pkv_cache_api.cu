@@ -157,7 +157,7 @@ bool tokens_ok(int64_t batch, int64_t tokens) { return batch >= 1 && tokens >= 1
 // ---------------------------------------------------------------- attention
 template <typename T, int D, int GT, bool POS>
 int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st) {
-  constexpr size_t kSmem = kCaWarps * CaWarp<T, D, GT, POS>::kRing + (sizeof(T) == 4 ? GT * D * 4 : 0);
+  constexpr size_t kSmem = kCaWarps * CaWarp<T, D, GT, POS>::kRing + (sizeof(T) == 4 ? 2 * GT * D * 4 : 0);
   constexpr int kPerSm = kSmem > 110 * 1024 ? 1 : 2;
   static bool attr_done[64] = {};          // the attribute is per device; setting it twice is harmless
   int dev = 0;

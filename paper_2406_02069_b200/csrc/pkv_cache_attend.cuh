@@ -6,8 +6,9 @@
 // What bounds it: every seen row is read once, 2 d elements for 4 d operations per query head, so the floor is the bytes of
 // the cache over the memory bandwidth; a call with few rows is a chain of latencies (lengths, table, rows, join).
 //   * The lengths are not known on the host, so the grid does not depend on them: as many CTAs as fit on the device at once,
-//     and the tiles (64 rows of one KV head and block of query heads) of the whole batch are dealt out to them in equal
-//     consecutive ranges.  A long sequence is then split over many CTAs, and a CTA takes many short ones in turn.
+//     which deal the batch's tiles (64 rows of one KV head and block of query heads) out among themselves (CaPlan).  A long
+//     sequence is split over many CTAs, and a CTA takes many short ones in turn, the next one's rows on their way while
+//     it finishes the one ahead.
 //   * A CTA that has all tiles of a head writes its output; otherwise it leaves (exponent, sum, weighted sum) in the workspace, and
 //     the last CTA of the head to arrive joins them in the order of the rows, so that equal calls give equal bits.
 //   * A warp takes tiles of 16 rows, kStages of them in shared memory or on their way by asynchronous copies.  A row that is
@@ -125,8 +126,7 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
 }
 
 // One warp's sums over rows first .. first + 15, first + kCaTile .. of a segment: weights' sums to z[GT], exponents that they
-// are relative to (-infinity: no seen row) to m[GT], weighted sums of V to acc[GT][D + 4], all in shared memory; acc is the warp's own
-// ring, whose rows are used up by then.
+// are relative to (-infinity: no seen row) to m[GT], weighted sums of V to acc[GT][D + 4], all in shared memory.
 template <typename T, int D, int GT, bool POS>
 struct CaWarp {
   static constexpr uint32_t ROW = D * sizeof(T), TILE = 16 * ROW;
@@ -166,7 +166,10 @@ struct CaSums {
   using X = Dec16<T>;
   static constexpr int KC = D / 32, VC = D / 64;
   uint4 q[KC];
-  float o[VC * 8][4];
+  // [channel octet's element][fragment rows g, g + 8]: channels of two of the octets.  Each tile's products are added to
+  // them on the fp32 pipe, which rounds to nearest; the tensor core's own accumulation cuts off, and over 131072 rows that
+  // came to 2e-6 of the output (4e-7 this way).
+  unsigned long long o[VC * 8][2];
   float m, z;                              // of head g % GT: m over the warp's rows, z over this lane's
   float slope;
 
@@ -178,7 +181,7 @@ struct CaSums {
       q[j] = there ? *reinterpret_cast<const uint4*>(q0 + g * p.q_sh + j * 32 + c * 8) : make_uint4(0, 0, 0, 0);
     slope = POS && p.slopes && there ? __ldg(p.slopes + hq + g) * 1.4426950408889634f : 0.f;
 #pragma unroll
-    for (int i = 0; i < VC * 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    for (int i = 0; i < VC * 8; ++i) o[i][0] = o[i][1] = 0ull;
     m = -INFINITY;
     z = 0.f;
   }
@@ -213,10 +216,12 @@ struct CaSums {
     if (__any_sync(0xffffffffu, mn > m)) {
       const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
       z *= corr;
+      const unsigned long long corr2 = pack2(corr, corr);
 #pragma unroll
-      for (int i = 0; i < VC * 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] *= corr;
+      for (int i = 0; i < VC * 8; ++i) {
+        o[i][0] = mul2(o[i][0], corr2);
+        o[i][1] = mul2(o[i][1], corr2);
+      }
     }
     m = mn;
     uint32_t a[2][2], low8[2];             // [rows 2c.. / 2c + 8..][fragment row g / g + 8]
@@ -252,12 +257,19 @@ struct CaSums {
         const uint32_t v2 = reinterpret_cast<const uint32_t*>(&v[2])[w], v3 = reinterpret_cast<const uint32_t*>(&v[3])[w];
         const uint32_t e0 = __byte_perm(v0, v1, 0x5410), e1 = __byte_perm(v2, v3, 0x5410);
         const uint32_t f0 = __byte_perm(v0, v1, 0x7632), f1 = __byte_perm(v2, v3, 0x7632);
-        X::mma(o[j * 8 + 2 * w], a[0][0], a[0][1], a[1][0], a[1][1], e0, e1);
-        X::mma(o[j * 8 + 2 * w + 1], a[0][0], a[0][1], a[1][0], a[1][1], f0, f1);
+        float d0[4] = {0.f, 0.f, 0.f, 0.f}, d1[4] = {0.f, 0.f, 0.f, 0.f};
+        X::mma(d0, a[0][0], a[0][1], a[1][0], a[1][1], e0, e1);
+        X::mma(d1, a[0][0], a[0][1], a[1][0], a[1][1], f0, f1);
         if (GT == 8) {
-          X::mma(o[j * 8 + 2 * w], low8[0], 0u, low8[1], 0u, e0, e1);
-          X::mma(o[j * 8 + 2 * w + 1], low8[0], 0u, low8[1], 0u, f0, f1);
+          X::mma(d0, low8[0], 0u, low8[1], 0u, e0, e1);
+          X::mma(d1, low8[0], 0u, low8[1], 0u, f0, f1);
         }
+        unsigned long long* to = o[j * 8 + 2 * w];
+        to[0] = add2(to[0], pack2(d0[0], d0[1]));
+        to[1] = add2(to[1], pack2(d0[2], d0[3]));
+        to = o[j * 8 + 2 * w + 1];
+        to[0] = add2(to[0], pack2(d1[0], d1[1]));
+        to[1] = add2(to[1], pack2(d1[2], d1[3]));
       }
     }
   }
@@ -277,7 +289,8 @@ struct CaSums {
         float t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float s0 = o[j * 8 + i][0] + o[j * 8 + i][2], s1 = o[j * 8 + i][1] + o[j * 8 + i][3];
+          float s0, s1;
+          unpack2(add2(o[j * 8 + i][0], o[j * 8 + i][1]), s0, s1);
           t[i] = (upper ? s1 : s0) + __shfl_xor_sync(0xffffffffu, upper ? s0 : s1, 16);
           special = fmaf(t[i], 0.f, special);
         }
@@ -291,8 +304,7 @@ struct CaSums {
         float t[2][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          t[0][i] = o[j * 8 + i][0] + o[j * 8 + i][2];
-          t[1][i] = o[j * 8 + i][1] + o[j * 8 + i][3];
+          unpack2(add2(o[j * 8 + i][0], o[j * 8 + i][1]), t[0][i], t[1][i]);
           special = fmaf(t[0][i], 0.f, special);
           special = fmaf(t[1][i], 0.f, special);
         }
@@ -428,27 +440,218 @@ __device__ __forceinline__ void ca_write(const CacheAttendParams& p, int64_t hea
   if (channel == 0 && p.lse) p.lse[head] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
 }
 
-// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory kCaWarps rings (+ GT * D floats in fp32).
+// Partial results of a block of query heads -> its output, by one CTA.  The first one is at `first`, the others at rest + 2,
+// rest + 4 ... rest + 2 more.  factors: shared memory for (more + 1) * GT floats.  A warp finds the factors of a head; then every
+// thread has four channels of a head and adds up the partials in the order of the rows, kAhead loads on their way at a time.
+// (One channel and one load at a time: 120 us for the 37 partials of 8 heads x 128 channels, now 4.)
+template <int D, int GT>
+__device__ __forceinline__ void ca_join(const CacheAttendParams& p, float* factors, int first, int more, int rest, int heads, int64_t head0) {
+  constexpr int kAhead = 8;
+  __shared__ float s_jm[GT], s_jz[GT];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto partial = [&](int i) { return p.partials + static_cast<int64_t>(i == 0 ? first : rest + 2 * i) * kCaPartial; };
+  for (int g = warp; g < heads; g += kCaWarps) {
+    float m = -INFINITY;
+    for (int i = lane; i <= more; i += 32) {
+      const float mi = __ldcg(partial(i) + GT * D + g);
+      factors[i * GT + g] = mi;
+      m = fmaxf(m, mi);
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+    float z = 0.f;
+    for (int i = lane; i <= more; i += 32) {
+      const float f = ca_factor(factors[i * GT + g], m);
+      factors[i * GT + g] = f;
+      z = fmaf(__ldcg(partial(i) + GT * D + GT + g), f, z);
+    }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) z += __shfl_xor_sync(0xffffffffu, z, s);
+    if (lane == 0) {
+      s_jm[g] = m;
+      s_jz[g] = z;
+    }
+  }
+  __syncthreads();
+  for (int o = threadIdx.x * 4; o < heads * D; o += kCaThreads * 4) {
+    const int g = o / D;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i <= more; i += kAhead) {
+      float4 x[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j <= more) x[j] = __ldcg(reinterpret_cast<const float4*>(partial(i + j) + o));
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i + j > more) continue;
+        const float f = factors[(i + j) * GT + g];
+        a.x = fmaf(x[j].x, f, a.x);
+        a.y = fmaf(x[j].y, f, a.y);
+        a.z = fmaf(x[j].z, f, a.z);
+        a.w = fmaf(x[j].w, f, a.w);
+      }
+    }
+    const float m = s_jm[g], z = s_jz[g];
+    const int channel = o - g * D;
+    ca_write(p, head0 + g, D, channel, m, z, a.x);
+    ca_write(p, head0 + g, D, channel + 1, m, z, a.y);
+    ca_write(p, head0 + g, D, channel + 2, m, z, a.z);
+    ca_write(p, head0 + g, D, channel + 3, m, z, a.w);
+  }
+}
+
+// How the tiles of a call are dealt out.  A unit is a block of query heads of one KV head of one sequence; s_off has the tiles of
+// a unit of the sequences ahead (at least one per sequence, whose rows may be none).
+//   * Where there are fewer units than CTAs (and it costs next to nothing): every unit in equal parts of at most `most` tiles, one part to a
+//     CTA, `most` as small as it can be.
+//   * Else equal consecutive ranges of all tiles.  Starting on a unit and handing over its sums takes a CTA about as long as kCaStart
+//     tiles, so that many are counted on top of each unit's own.
+// (64 sequences of 129 to 4096 rows, 32 / 8 heads: 120 us without the count, equal lengths 95.  Eight sequences of 300 to 700 rows:
+// 14.6 us in equal ranges, where nearly every CTA has the end of one unit and the start of another.)
+constexpr int kCaStart = 2;
+constexpr int kCaSpare = 3;                // tiles that parts may have more than equal ranges would
+
+struct CaSegment {
+  int b, unit;                             // unit of the sequence: KV head * head_blocks + block
+  int tile0, tile1;
+  bool whole;                              // the unit's only segment
+  int slot;                                // where this segment's partial result goes
+  int first, rest, more;                   // where the unit's are: the first one, and rest + 2 .. rest + 2 more
+};
+
+struct CaPlan {
+  const int32_t* off;
+  int batch, per_seq;                      // units of a sequence
+  int64_t begin, end, total;               // this CTA's range, and all of it (equal ranges)
+  int64_t at;
+  int b;
+  int parts_of;                            // > 0: parts of at most so many tiles
+  bool done;
+
+  __device__ __forceinline__ int64_t start_of(int64_t cta) const { return total * cta / gridDim.x; }
+  __device__ __forceinline__ int64_t owner(int64_t tile) const { return ((tile + 1) * gridDim.x - 1) / total; }
+  __device__ __forceinline__ int64_t ahead(int s) const { return static_cast<int64_t>(off[s] + kCaStart * s) * per_seq; }
+
+  // All warps come to the same plan.
+  __device__ __forceinline__ void make(const int32_t* s_off, int sequences, int units_per_seq) {
+    off = s_off;
+    batch = sequences;
+    per_seq = units_per_seq;
+    done = false;
+    parts_of = 0;
+    const int lane = threadIdx.x & 31, ctas = gridDim.x;
+    const int64_t units = static_cast<int64_t>(batch) * per_seq, tiles = static_cast<int64_t>(off[batch]) * per_seq;
+    if (units <= ctas) {
+      auto parts = [&](int64_t most) {
+        unsigned sum = 0;
+        for (int s = lane; s < batch; s += 32) sum += static_cast<unsigned>((off[s + 1] - off[s] + most - 1) / most);
+        return static_cast<int64_t>(__reduce_add_sync(0xffffffffu, sum)) * per_seq;
+      };
+      int64_t lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
+      hi = max(lo, hi);                    // parts of hi tiles fit: there are fewer than tiles / hi + units of them
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (parts(mid) <= ctas) hi = mid;
+        else lo = mid + 1;
+      }
+      if (hi * ctas <= tiles + static_cast<int64_t>(kCaSpare) * ctas) parts_of = static_cast<int>(hi);
+    }
+    if (parts_of) return;
+    total = ahead(batch);
+    at = begin = start_of(blockIdx.x);
+    end = start_of(blockIdx.x + 1);
+    b = 0;
+    for (int step = 512; step > 0; step >>= 1)                   // the last sequence that starts at or before `at`
+      if (b + step < batch && ahead(b + step) <= at) b += step;
+  }
+
+  // The next segment of this CTA, false behind the last one.
+  __device__ __forceinline__ bool next(CaSegment* s) {
+    if (parts_of) {
+      if (done) return false;
+      done = true;
+      const int lane = threadIdx.x & 31;
+      int64_t run = 0;                     // parts of the sequences ahead
+      for (int s0 = 0; s0 < batch; s0 += 32) {
+        const int x = s0 + lane < batch ? (off[s0 + lane + 1] - off[s0 + lane] + parts_of - 1) / parts_of : 0;
+        int sum = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, (run + sum) * per_seq > static_cast<int64_t>(blockIdx.x));
+        if (past) {
+          const int l = __ffs(past) - 1, parts = __shfl_sync(0xffffffffu, x, l);
+          const int64_t in_seq = blockIdx.x - (run + __shfl_sync(0xffffffffu, sum, l) - parts) * per_seq;
+          s->b = s0 + l;
+          const int tiles = off[s->b + 1] - off[s->b];
+          s->unit = static_cast<int>(in_seq / parts);
+          const int k = static_cast<int>(in_seq) - s->unit * parts;
+          s->tile0 = static_cast<int>(static_cast<int64_t>(tiles) * k / parts);
+          s->tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (k + 1) / parts);
+          s->whole = parts == 1;
+          s->slot = 2 * blockIdx.x;
+          s->first = s->rest = 2 * (blockIdx.x - k);
+          s->more = parts - 1;
+          return true;
+        }
+        run += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      return false;                        // more CTAs than parts
+    }
+    while (at < end) {
+      while (at >= ahead(b + 1)) ++b;
+      const int tiles = off[b + 1] - off[b], counted = tiles + kCaStart;
+      const int64_t in_seq = at - ahead(b);
+      s->b = b;
+      s->unit = static_cast<int>(in_seq / counted);
+      const int v0 = static_cast<int>(in_seq - static_cast<int64_t>(s->unit) * counted);
+      const int v1 = static_cast<int>(min(static_cast<int64_t>(counted), v0 + (end - at)));
+      const int64_t unit0 = at - v0;
+      at += v1 - v0;
+      s->tile0 = max(0, v0 - kCaStart);
+      s->tile1 = max(0, v1 - kCaStart);
+      if (s->tile0 == s->tile1) continue;
+      s->whole = s->tile0 == 0 && s->tile1 == tiles;
+      if (!s->whole) {
+        // a CTA has at most one unit that it did not start (place 0) and one that it does not finish (place 1)
+        const int64_t c0 = owner(unit0 + kCaStart);
+        s->more = static_cast<int>(owner(unit0 + counted - 1) - c0);
+        s->slot = 2 * blockIdx.x + (begin <= unit0 ? 1 : 0);
+        s->rest = static_cast<int>(2 * c0);
+        s->first = s->rest + (start_of(c0) <= unit0 ? 1 : 0);
+      }
+      return true;
+    }
+    return false;
+  }
+};
+
+// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory kCaWarps rings (+ 2 GT * D floats in fp32).
 template <typename T, int D, int GT, bool POS>
 __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
   using W = CaWarp<T, D, GT, POS>;
   using Sums = CaSums<T, D, GT, POS>;
-  static_assert(GT * W::HEAD * 4 <= W::kRing, "a warp's sums fit its ring");
+  constexpr uint32_t kSlot = 2 * W::TILE;
+  static_assert(GT * W::HEAD * 4 <= kSlot, "a warp's sums fit the last slot of its ring");
   extern __shared__ __align__(128) uint8_t ca_smem[];
-  __shared__ int32_t s_off[PKV_MAX_CACHE_BATCH + 1];             // tiles of a head of the sequences ahead
+  __shared__ int32_t s_off[PKV_MAX_CACHE_BATCH + 1];             // tiles of a unit of the sequences ahead
   __shared__ int32_t s_scan[kCaWarps];
   __shared__ float s_m[kCaWarps][GT], s_z[kCaWarps][GT];
+  __shared__ float s_factors[kCaMaxGrid * GT];
   __shared__ int32_t s_last;
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int most = static_cast<int>(min(static_cast<int64_t>(p.max_pages) * p.page_size, static_cast<int64_t>(INT32_MAX - kCaTile)));
+  const int most = static_cast<int>(static_cast<int64_t>(p.max_pages) * p.page_size);      // the host keeps it below 2^30
   pdl_wait();
 
-  // ---- tiles of every sequence (at least one, whose rows may be none) and their running sum
+  // ---- tiles of every sequence and their running sum
   {
     constexpr int PER = PKV_MAX_CACHE_BATCH / kCaThreads;
     int mine[PER], sum = 0;
     const int per = (p.batch + kCaThreads - 1) / kCaThreads;     // consecutive sequences of a thread
+#pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int b = tid * per + i;
       mine[i] = 0;
@@ -465,6 +668,7 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
     __syncthreads();
     for (int w = 0; w < warp; ++w) run += s_scan[w];
     run -= sum;
+#pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int b = tid * per + i;
       if (i < per && b < p.batch) s_off[b] = run;
@@ -473,89 +677,93 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
     if (tid == kCaThreads - 1) s_off[p.batch] = run;
     __syncthreads();
   }
-  const int per_seq = p.num_kv_heads * p.head_blocks;
-  const int64_t total = static_cast<int64_t>(s_off[p.batch]) * per_seq;
-  const int64_t ctas = min(static_cast<int64_t>(gridDim.x), total);
-  if (blockIdx.x >= ctas) return;
-  auto range_begin = [&](int64_t cta) { return total * cta / ctas; };
-  auto owner = [&](int64_t tile) { return ((tile + 1) * ctas - 1) / total; };
-  const int64_t begin = range_begin(blockIdx.x), end = range_begin(blockIdx.x + 1);
+  CaPlan plan;
+  plan.make(s_off, p.batch, p.num_kv_heads * p.head_blocks);
+  CaSegment seg;
+  bool have = plan.next(&seg);
+  if (!have) return;
+
   const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ca_smem)) + warp * static_cast<uint32_t>(W::kRing);
-  float* acc = reinterpret_cast<float*>(ca_smem + warp * W::kRing);
-
-  int b = 0;
-  for (int64_t at = begin; at < end;) {
-    // ---- the segment: tiles tile0 .. tile1 - 1 of one block of query heads
-    while (at >= static_cast<int64_t>(s_off[b + 1]) * per_seq) ++b;
-    const int tiles = s_off[b + 1] - s_off[b];
-    const int64_t in_seq = at - static_cast<int64_t>(s_off[b]) * per_seq;
-    const int unit = static_cast<int>(in_seq / tiles), tile0 = static_cast<int>(in_seq - static_cast<int64_t>(unit) * tiles);
-    const int tile1 = static_cast<int>(min(static_cast<int64_t>(tiles), tile0 + (end - at)));
-    const int h = unit / p.head_blocks, g0 = (unit - h * p.head_blocks) * GT;
-    const int heads = min(GT, p.group - g0);
-    const int hq = h * p.group + g0;
-    const T* q0 = static_cast<const T*>(p.q) + b * p.q_sb + hq * p.q_sh;
-    const int n = min(max(__ldg(p.lens + b), 0), most);
-    CaRows<POS> rows;
-    rows.table = p.table + (static_cast<int64_t>(b) * p.num_kv_heads + h) * p.max_pages;
-    rows.rows = min(n, tile1 * kCaTile);
-    rows.q_pos = POS ? __ldg(p.q_pos + b) : 0;
-    const int first = tile0 * kCaTile + warp * 16;
-
-    // ---- copies of the first tiles
-    uint32_t seen[kCaStages], far[kCaStages];
-    {
-      int64_t mine[kCaStages];
+  constexpr uint32_t kAcc = (kCaStages - 1) * kSlot;             // the warp's sums: in the last slot of its ring
+  CaRows<POS> rows;
+  const T* q0;
+  int first, heads, hq;
+  uint32_t seen[kCaStages], far[kCaStages];                      // of the tiles in the ring, oldest first
+  int64_t mine_last;                                             // where the rows of the last slot's tile lie
+  int q_buffer = 0;
+  Sums sums;
+  auto look_up = [&](int t0, uint32_t* f) { return ca_look_up<POS>(p, rows, t0 + (lane & 15), lane < 16, f); };
+  auto copy_in = [&](uint32_t slot, uint32_t there, int64_t mine) {
+    if (there) W::copy_tile(p, ring + slot, mine);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // Starts on a segment: the tiles of all slots but the last one are on their way.
+  auto begin = [&]() {
+    const int h = seg.unit / p.head_blocks, g0 = (seg.unit - h * p.head_blocks) * GT;
+    heads = min(GT, p.group - g0);
+    hq = h * p.group + g0;
+    q0 = static_cast<const T*>(p.q) + seg.b * p.q_sb + hq * p.q_sh;
+    rows.table = p.table + (static_cast<int64_t>(seg.b) * p.num_kv_heads + h) * p.max_pages;
+    rows.rows = min(min(max(__ldg(p.lens + seg.b), 0), most), seg.tile1 * kCaTile);
+    rows.q_pos = POS ? __ldg(p.q_pos + seg.b) : 0;
+    first = seg.tile0 * kCaTile + warp * 16;
+    int64_t mine[kCaStages];
 #pragma unroll
-      for (int s = 0; s < kCaStages; ++s) mine[s] = ca_look_up<POS>(p, rows, first + s * kCaTile + (lane & 15), lane < 16, &far[s]);
+    for (int s = 0; s < kCaStages; ++s) mine[s] = look_up(first + s * kCaTile, &far[s]);
 #pragma unroll
-      for (int s = 0; s < kCaStages; ++s) {
-        seen[s] = __ballot_sync(0xffffffffu, mine[s] >= 0);
-        if (seen[s]) W::copy_tile(p, ring + s * (2 * W::TILE), mine[s]);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      }
+    for (int s = 0; s < kCaStages; ++s) {
+      seen[s] = __ballot_sync(0xffffffffu, mine[s] >= 0);
+      if (s < kCaStages - 1) copy_in(s * kSlot, seen[s], mine[s]);
     }
-    uint32_t far_next;
-    int64_t next = ca_look_up<POS>(p, rows, first + kCaStages * kCaTile + (lane & 15), lane < 16, &far_next);
-    const float* q_f = nullptr;
+    mine_last = mine[kCaStages - 1];
     if constexpr (sizeof(T) == 4) {
-      float* q_shared = reinterpret_cast<float*>(ca_smem + kCaWarps * W::kRing);
+      float* q_shared = reinterpret_cast<float*>(ca_smem + kCaWarps * W::kRing) + q_buffer * (GT * D);
+      q_buffer ^= 1;
       for (int i = tid; i < GT * D; i += kCaThreads) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
-      __syncthreads();
-      q_f = q_shared;
+      sums.start(p, q_shared, heads, hq);
+    } else {
+      sums.start(p, q0, heads, hq);
     }
-    Sums sums;
-    if constexpr (sizeof(T) == 4) sums.start(p, q_f, heads, hq);
-    else sums.start(p, q0, heads, hq);
+  };
+  begin();
+  while (true) {
+    if constexpr (sizeof(T) == 4) __syncthreads();               // the queries are there
+    copy_in(kAcc, seen[kCaStages - 1], mine_last);
+    uint32_t far_next;
+    int64_t next = look_up(first + kCaStages * kCaTile, &far_next);
 
     // ---- the warp's rows
-    for (int t0 = first; t0 < rows.rows;) {
+    uint32_t slot = 0;
+    for (int t0 = first; t0 < rows.rows; t0 += kCaTile) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kCaStages - 1) : "memory");
+      __syncwarp();
+      if (seen[0]) sums.step(p, ring + slot, ring + slot + W::TILE, seen[0], far[0]);
+      __syncwarp();                        // the tile has been read
 #pragma unroll
-      for (int slot = 0; slot < kCaStages; ++slot) {
-        if (t0 >= rows.rows) break;        // (uniform over the warp)
-        asm volatile("cp.async.wait_group %0;" ::"n"(kCaStages - 1) : "memory");
-        __syncwarp();
-        const uint32_t k_at = ring + slot * (2 * W::TILE);
-        if (seen[slot]) sums.step(p, k_at, k_at + W::TILE, seen[slot], far[slot]);
-        __syncwarp();                      // the tile has been read
-        seen[slot] = __ballot_sync(0xffffffffu, next >= 0);
-        far[slot] = far_next;
-        if (seen[slot]) W::copy_tile(p, k_at, next);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        t0 += kCaTile;
-        next = ca_look_up<POS>(p, rows, t0 + kCaStages * kCaTile + (lane & 15), lane < 16, &far_next);
+      for (int s = 0; s + 1 < kCaStages; ++s) {
+        seen[s] = seen[s + 1];
+        far[s] = far[s + 1];
       }
+      seen[kCaStages - 1] = __ballot_sync(0xffffffffu, next >= 0);
+      far[kCaStages - 1] = far_next;
+      copy_in(slot, seen[kCaStages - 1], next);
+      next = look_up(t0 + (kCaStages + 1) * kCaTile, &far_next);
+      slot = slot == kAcc ? 0 : slot + kSlot;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncwarp();
-    sums.finish(p, rows, q0, heads, first, acc, s_m[warp], s_z[warp]);
-    __syncthreads();
+    sums.finish(p, rows, q0, heads, first, reinterpret_cast<float*>(ca_smem + warp * W::kRing + kAcc), s_m[warp], s_z[warp]);
 
-    // ---- the warps' sums; then the output, or a partial result that the head's last CTA joins with the others
-    const int64_t head0 = static_cast<int64_t>(b) * p.num_kv_heads * p.group + hq;
-    const bool whole = tile0 == 0 && tile1 == tiles;
-    float* part = p.partials + (2 * static_cast<int64_t>(blockIdx.x) + (at > begin ? 1 : 0)) * kCaPartial;
-    for (int o = tid; o < heads * D; o += kCaThreads) {
+    // ---- the next segment's rows start on their way, then the warps' sums meet
+    const CaSegment was = seg;
+    const int heads_was = heads;
+    const int64_t head0 = static_cast<int64_t>(was.b) * p.num_kv_heads * p.group + hq;
+    have = plan.next(&seg);
+    if (have) begin();
+    __syncthreads();
+    // the output, or a partial result that the unit's last CTA joins with the others
+    float* part = p.partials + static_cast<int64_t>(was.slot) * kCaPartial;
+    for (int o = tid; o < heads_was * D; o += kCaThreads) {
       const int g = o / D, channel = o - g * D;
       float m = s_m[0][g];
 #pragma unroll
@@ -565,9 +773,9 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
       for (int w = 0; w < kCaWarps; ++w) {
         const float f = ca_factor(s_m[w][g], m);
         z = fmaf(s_z[w][g], f, z);
-        a = fmaf(reinterpret_cast<const float*>(ca_smem + w * W::kRing)[g * W::HEAD + channel], f, a);
+        a = fmaf(reinterpret_cast<const float*>(ca_smem + w * W::kRing + kAcc)[g * W::HEAD + channel], f, a);
       }
-      if (whole) {
+      if (was.whole) {
         ca_write(p, head0 + g, D, channel, m, z, a);
       } else {
         __stcg(part + o, a);
@@ -577,37 +785,20 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
         }
       }
     }
-    if (!whole) {
-      const int64_t unit0 = at - tile0, c0 = owner(unit0), c1 = owner(unit0 + tiles - 1);
-      int32_t* counter = p.counters + static_cast<int64_t>(b) * per_seq + unit;
+    if (!was.whole) {
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        const int before = atomicAdd(counter, 1);
-        s_last = before == static_cast<int>(c1 - c0);
+        int32_t* counter = p.counters + static_cast<int64_t>(was.b) * plan.per_seq + was.unit;
+        s_last = atomicAdd(counter, 1) == was.more;
         if (s_last) *counter = 0;          // everybody has arrived: ready for the next call
         __threadfence();
       }
       __syncthreads();
-      if (s_last) {
-        for (int o = tid; o < heads * D; o += kCaThreads) {
-          const int g = o / D, channel = o - g * D;
-          float m = -INFINITY, z = 0.f, a = 0.f;
-          for (int64_t c = c0; c <= c1; ++c) {                   // in the order of the rows
-            const float* other = p.partials + (2 * c + (range_begin(c) < unit0 ? 1 : 0)) * kCaPartial;
-            const float mo = __ldcg(other + GT * D + g);
-            const float mn = fmaxf(m, mo);
-            const float f = ca_factor(m, mn), fo = ca_factor(mo, mn);
-            z = fmaf(z, f, __ldcg(other + GT * D + GT + g) * fo);
-            a = fmaf(a, f, __ldcg(other + o) * fo);
-            m = mn;
-          }
-          ca_write(p, head0 + g, D, channel, m, z, a);
-        }
-      }
+      if (s_last) ca_join<D, GT>(p, s_factors, was.first, was.more, was.rest, heads_was, head0);
     }
-    __syncthreads();                       // the sums have been read: the rings may be filled again
-    at += tile1 - tile0;
+    if (!have) return;
+    __syncthreads();                       // the sums have been read: the last slot may be filled
   }
 }
 
