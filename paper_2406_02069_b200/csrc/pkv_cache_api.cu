@@ -1,5 +1,6 @@
 // Host side of the growing cache: rotary plans, argument checks, workspace carving and launches of the calls that include/pyramidkv.h
 // lists under "A cache that grows behind the compressed prompt".
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -157,22 +158,23 @@ bool tokens_ok(int64_t batch, int64_t tokens) { return batch >= 1 && tokens >= 1
 // ---------------------------------------------------------------- attention
 template <typename T, int D, int GT, bool POS>
 int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st) {
-  constexpr size_t kSmem = kCaWarps * CaWarp<T, D, GT, POS>::kRing + (sizeof(T) == 4 ? 2 * GT * D * 4 : 0);
-  constexpr int kPerSm = kSmem > 110 * 1024 ? 1 : 2;
-  static bool attr_done[64] = {};          // the attribute is per device; setting it twice is harmless
+  constexpr size_t kSmem = kCaWarps<T> * CaWarp<T, D, GT, POS>::kRing + (sizeof(T) == 4 ? 2 * GT * (D + 4) * 4 : 0);
+  static std::atomic<int> per_sm[64];      // CTAs that an SM holds, once the kernel's shared memory is set up on a device
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return PKV_ERR_CUDA;
-  if (dev >= 64 || !attr_done[dev]) {
-    if (cudaFuncSetAttribute(cache_attend_kernel<T, D, GT, POS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)) != cudaSuccess)
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return PKV_ERR_CUDA;
+  int fit = per_sm[dev].load(std::memory_order_acquire);
+  if (!fit) {
+    if (cudaFuncSetAttribute(cache_attend_kernel<T, D, GT, POS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&fit, cache_attend_kernel<T, D, GT, POS>, kCaThreads<T>, kSmem) != cudaSuccess || fit < 1)
       return PKV_ERR_CUDA;
-    if (dev < 64) attr_done[dev] = true;
+    per_sm[dev].store(fit, std::memory_order_release);
   }
   const int sms = device_sm_count();
   if (sms <= 0) return PKV_ERR_CUDA;
   // no more CTAs than there can be tiles
   const int64_t tiles = (max_rows + kCaTile - 1) / kCaTile * p.batch * p.num_kv_heads * p.head_blocks;
-  const int grid = static_cast<int>(std::min<int64_t>(std::min(kCaMaxGrid, sms * kPerSm), tiles));
-  launch_pdl(cache_attend_kernel<T, D, GT, POS>, dim3(grid), dim3(kCaThreads), kSmem, st, p);
+  const int grid = static_cast<int>(std::min<int64_t>(std::min(kCaMaxGrid, sms * fit), tiles));
+  launch_pdl(cache_attend_kernel<T, D, GT, POS>, dim3(grid), dim3(kCaThreads<T>), kSmem, st, p);
   return check_launch();
 }
 
@@ -427,6 +429,9 @@ int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cac
   p.max_pages = cache->max_pages;
   p.page_size = cache->page_size;
   p.num_pages = cache->num_pages;
+  p.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (cache->page_size == 1 << i) p.page_shift = i;
   p.window = o.window;
   p.prefix = o.prefix;
   const double log2e = 1.4426950408889634, scale = o.scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(cfg->head_dim)) : o.scale;

@@ -24,10 +24,16 @@
 
 namespace pkv {
 
-constexpr int kCaWarps = 4;
-constexpr int kCaThreads = kCaWarps * 32;
-constexpr int kCaTile = kCaWarps * 16;     // rows of a tile: 16 to a warp
+constexpr int kCaTile = 64;                // rows of a tile, shared by the warps of a CTA
 constexpr int kCaStages = 3;               // a warp's tiles in shared memory or on their way
+// Warps of a CTA: four with 16 rows each of 16-bit types, eight with 8 rows each in fp32, where a row takes twice the bytes and
+// several times the instructions.
+template <typename T>
+constexpr int kCaWarps = sizeof(T) == 4 ? 8 : 4;
+template <typename T>
+constexpr int kCaThreads = kCaWarps<T> * 32;
+template <typename T>
+constexpr int kCaRows = kCaTile / kCaWarps<T>;
 constexpr int kCaMaxGrid = 2 * 160;        // CTAs at most (sizes the partial sums in the workspace)
 constexpr int kCaMaxHeads = 8;             // query heads of a CTA at most
 // Floats of one partial result: sums, then exponents, then weights' sums.
@@ -50,6 +56,7 @@ struct CacheAttendParams {
   float* partials;                         // [2 * gridDim.x][kCaPartial]
   int32_t batch, num_kv_heads, group, head_blocks;
   int32_t max_pages, page_size, num_pages;
+  int32_t page_shift;                      // log2(page_size), -1 if it is no power of two
   int32_t window, prefix;
   float scale_log2;                        // log2(e) scale; with a cap scale / cap
   float cap_log2;                          // log2(e) cap, 0: no cap
@@ -70,24 +77,24 @@ struct CaRows {
   int32_t q_pos;
 };
 
-// Where row r lies (in rows of the pool), -1 if it is not seen; *far: p - p_r.
+// Row r's place in the pool, counted in rows; -1 if it has none.
 template <bool POS>
-__device__ __forceinline__ int64_t ca_look_up(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report, uint32_t* far) {
-  *far = 0;
+__device__ __forceinline__ int64_t ca_place(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report) {
   if (r >= s.rows) return -1;
-  const int page = __ldg(s.table + r / p.page_size);
+  const int j = p.page_shift >= 0 ? r >> p.page_shift : r / p.page_size;
+  const int page = __ldg(s.table + j);
   if (page < 0 || page >= p.num_pages) {
     if (report) atomicOr(p.status, kStatusBadPage);
     return -1;
   }
-  const int64_t at = static_cast<int64_t>(page) * p.page_size + r % p.page_size;
-  if (POS) {
-    const int pos = __ldg(p.pos_pool + at);
-    *far = static_cast<uint32_t>(s.q_pos) - static_cast<uint32_t>(pos);       // positions may be 2^31 apart and more
-    if (pos > s.q_pos) return -1;
-    if (p.window > 0 && *far >= static_cast<uint32_t>(p.window) && pos >= p.prefix) return -1;
-  }
-  return at;
+  return static_cast<int64_t>(page) * p.page_size + (r - j * p.page_size);
+}
+
+// Whether the row at a place is seen, by its position; *far: p - p_r.
+template <bool POS>
+__device__ __forceinline__ bool ca_seen(const CacheAttendParams& p, const CaRows<POS>& s, int pos, uint32_t* far) {
+  *far = static_cast<uint32_t>(s.q_pos) - static_cast<uint32_t>(pos);         // positions may be 2^31 apart and more
+  return pos <= s.q_pos && (p.window == 0 || *far < static_cast<uint32_t>(p.window) || pos < p.prefix);
 }
 
 // Sums of one query head over the warp's rows on the fp32 pipe, for rows that hold infinities or NaN:
@@ -106,10 +113,10 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
 #pragma unroll 1
   for (int t0 = first; t0 < s.rows; t0 += kCaTile)
 #pragma unroll 1
-    for (int r = t0; r < min(t0 + 16, s.rows); ++r) {
-      uint32_t far;
-      const int64_t at = ca_look_up<POS>(p, s, r, false, &far);
-      if (at < 0) continue;
+    for (int r = t0; r < min(t0 + kCaRows<T>, s.rows); ++r) {
+      uint32_t far = 0;
+      const int64_t at = ca_place<POS>(p, s, r, false);
+      if (at < 0 || (POS && !ca_seen<POS>(p, s, __ldg(p.pos_pool + at), &far))) continue;
       const T* k = static_cast<const T*>(p.k_pool) + at * D + lane * PER;
       const T* v = static_cast<const T*>(p.v_pool) + at * D + lane * PER;
       float dot = 0.f;
@@ -125,11 +132,12 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
   for (int c = 0; c < PER; ++c) acc[lane * PER + c] = a[c];
 }
 
-// One warp's sums over rows first .. first + 15, first + kCaTile .. of a segment: weights' sums to z[GT], exponents that they
+// One warp's sums over rows first .. first + kCaRows - 1, first + kCaTile .. of a segment: weights' sums to z[GT], exponents that they
 // are relative to (-infinity: no seen row) to m[GT], weighted sums of V to acc[GT][D + 4], all in shared memory.
 template <typename T, int D, int GT, bool POS>
 struct CaWarp {
-  static constexpr uint32_t ROW = D * sizeof(T), TILE = 16 * ROW;
+  static constexpr int TR = kCaRows<T>;                          // rows of the warp's tile
+  static constexpr uint32_t ROW = D * sizeof(T), TILE = TR * ROW;
   static constexpr int PIECES = ROW / 16;                        // 16-byte pieces of a row: 8, 16 or 32
   static constexpr int ROWS_AT_ONCE = 32 / PIECES;
   static constexpr int HEAD = D + 4;                             // floats from a head's sums to the next one's
@@ -148,7 +156,7 @@ struct CaWarp {
   __device__ __forceinline__ static void copy_tile(const CacheAttendParams& p, uint32_t to_tile, int64_t mine) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int s = 0; s < 16 / ROWS_AT_ONCE; ++s) {
+    for (int s = 0; s < TR / ROWS_AT_ONCE; ++s) {
       const int r = s * ROWS_AT_ONCE + lane / PIECES, piece = lane % PIECES;
       const int64_t at = __shfl_sync(0xffffffffu, mine, r);
       const int64_t from = (at >= 0 ? at : 0) * D + piece * (16 / static_cast<int>(sizeof(T)));
@@ -333,36 +341,35 @@ struct CaSums {
   }
 };
 
-// fp32 rows.  Lane l has channels of half l / 16 of row l % 16 for the dot products, and channels 4 (l % PIECES) .. of the rows of
+// fp32 rows.  Lane l has channels of quarter l / 8 of row l % 8 for the dot products, and channels 4 (l % PIECES) .. of the rows of
 // parity l / PIECES (all rows where a row has 32 pieces) for the weighted sums.
 template <int D, int GT, bool POS>
 struct CaSums<float, D, GT, POS> {
   using W = CaWarp<float, D, GT, POS>;
   static constexpr int PIECES = W::PIECES, VR = W::ROWS_AT_ONCE;
+  static_assert(W::TR == 8, "");
   const float* q0;                         // shared memory: [GT][D], zeros for heads that are not there
-  float o[GT][4];
+  unsigned long long o[GT][2];
   float m[GT], z[GT];                      // m the same in all lanes; z of this lane's row
-  float slope[GT];
 
-  __device__ __forceinline__ void start(const CacheAttendParams& p, const float* q_shared, int heads, int hq) {
+  __device__ __forceinline__ void start(const CacheAttendParams&, const float* q_shared, int, int) {
     q0 = q_shared;
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
-      slope[g] = POS && p.slopes && g < heads ? __ldg(p.slopes + hq + g) * 1.4426950408889634f : 0.f;
-      o[g][0] = o[g][1] = o[g][2] = o[g][3] = 0.f;
+      o[g][0] = o[g][1] = 0ull;
       m[g] = -INFINITY;
       z[g] = 0.f;
     }
   }
 
   __device__ __forceinline__ void step(const CacheAttendParams& p, uint32_t k_at, uint32_t v_at, uint32_t seen, uint32_t far) {
-    const int lane = threadIdx.x & 31, row = lane & 15, part = lane >> 4;
+    const int lane = threadIdx.x & 31, row = lane & 7, part = lane >> 3;
     unsigned long long d2[GT][2];
 #pragma unroll
     for (int g = 0; g < GT; ++g) d2[g][0] = d2[g][1] = 0ull;
 #pragma unroll
-    for (int j = 0; j < PIECES / 2; ++j) {
-      const int piece = part * (PIECES / 2) + j;
+    for (int j = 0; j < PIECES / 4; ++j) {
+      const int piece = part * (PIECES / 4) + j;
       const uint4 raw = dec_lds16(k_at + row * W::ROW + W::k_place(row, piece));
       const unsigned long long k0 = pack2(__uint_as_float(raw.x), __uint_as_float(raw.y));
       const unsigned long long k1 = pack2(__uint_as_float(raw.z), __uint_as_float(raw.w));
@@ -374,39 +381,44 @@ struct CaSums<float, D, GT, POS> {
       }
     }
     const bool live = (seen >> row) & 1u;
-    const float d = POS ? __uint2float_rn(far) : 0.f;             // lane l has row l % 16's
+    const float d = POS ? __uint2float_rn(far) : 0.f;             // lane l has row l % 8's
     float w[GT];
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
       float a, b;
       unpack2(add2(d2[g][0], d2[g][1]), a, b);
       float dot = a + b;
+      dot += __shfl_xor_sync(0xffffffffu, dot, 8);
       dot += __shfl_xor_sync(0xffffffffu, dot, 16);
-      const float x = live ? ca_logit(p, dot, slope[g], d) : -INFINITY;
+      const float slope = POS ? q0[GT * D + g] : 0.f;             // (behind the queries)
+      const float x = live ? ca_logit(p, dot, slope, d) : -INFINITY;
       float mx = x;
 #pragma unroll
-      for (int s = 8; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+      for (int s = 4; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
       const float mn = fmaxf(m[g], mx);
       if (mn > m[g]) {                     // the same in all lanes
         const float corr = m[g] == -INFINITY ? 0.f : exp2f(m[g] - mn);
+        const unsigned long long corr2 = pack2(corr, corr);
         z[g] *= corr;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[g][e] *= corr;
+        o[g][0] = mul2(o[g][0], corr2);
+        o[g][1] = mul2(o[g][1], corr2);
         m[g] = mn;
       }
       w[g] = exp2f(x - (mn == -INFINITY ? 0.f : mn));
       z[g] += w[g];
     }
 #pragma unroll
-    for (int r0 = 0; r0 < 16; r0 += VR) {
+    for (int r0 = 0; r0 < W::TR; r0 += VR) {
       const int r = r0 + lane / PIECES;
       const uint4 raw = dec_lds16(v_at + r * W::ROW + W::v_place(r, lane % PIECES));
-      const float v[4] = {__uint_as_float(raw.x), __uint_as_float(raw.y), __uint_as_float(raw.z), __uint_as_float(raw.w)};
+      const unsigned long long v0 = pack2(__uint_as_float(raw.x), __uint_as_float(raw.y));
+      const unsigned long long v1 = pack2(__uint_as_float(raw.z), __uint_as_float(raw.w));
 #pragma unroll
       for (int g = 0; g < GT; ++g) {
         const float wr = __shfl_sync(0xffffffffu, w[g], r);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[g][e] = fmaf(wr, v[e], o[g][e]);
+        const unsigned long long w2 = pack2(wr, wr);
+        o[g][0] = fma2(w2, v0, o[g][0]);
+        o[g][1] = fma2(w2, v1, o[g][1]);
       }
     }
   }
@@ -418,11 +430,14 @@ struct CaSums<float, D, GT, POS> {
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
 #pragma unroll
-      for (int s = 8; s > 0; s >>= 1) z[g] += __shfl_xor_sync(0xffffffffu, z[g], s);
+      for (int s = 4; s > 0; s >>= 1) z[g] += __shfl_xor_sync(0xffffffffu, z[g], s);
+      float t[4];
+      unpack2(o[g][0], t[0], t[1]);
+      unpack2(o[g][1], t[2], t[3]);
+      if (VR == 2)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (VR == 2) o[g][e] += __shfl_xor_sync(0xffffffffu, o[g][e], 16);
-      if (lane < PIECES) *reinterpret_cast<float4*>(acc + g * W::HEAD + lane * 4) = make_float4(o[g][0], o[g][1], o[g][2], o[g][3]);
+        for (int e = 0; e < 4; ++e) t[e] += __shfl_xor_sync(0xffffffffu, t[e], 16);
+      if (lane < PIECES) *reinterpret_cast<float4*>(acc + g * W::HEAD + lane * 4) = make_float4(t[0], t[1], t[2], t[3]);
       if (lane == 0) {
         m_out[g] = m[g];
         z_out[g] = z[g];
@@ -441,28 +456,30 @@ __device__ __forceinline__ void ca_write(const CacheAttendParams& p, int64_t hea
 }
 
 // Partial results of a block of query heads -> its output, by one CTA.  The first one is at `first`, the others at rest + 2,
-// rest + 4 ... rest + 2 more.  factors: shared memory for (more + 1) * GT floats.  A warp finds the factors of a head; then every
+// rest + 4 ... rest + 2 more.  The factors go to shared memory, to the last slots of the warps' rings in turn.  A warp finds the factors of a head; then every
 // thread has four channels of a head and adds up the partials in the order of the rows, kAhead loads on their way at a time.
 // (One channel and one load at a time: 120 us for the 37 partials of 8 heads x 128 channels, now 4.)
-template <int D, int GT>
-__device__ __forceinline__ void ca_join(const CacheAttendParams& p, float* factors, int first, int more, int rest, int heads, int64_t head0) {
+template <typename T, int D, int GT>
+__device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* last_slots, uint32_t ring, int first, int more, int rest, int heads,
+                                        int64_t head0) {
   constexpr int kAhead = 8;
   __shared__ float s_jm[GT], s_jz[GT];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto factor = [&](int i) -> float* { return reinterpret_cast<float*>(last_slots + (i % kCaWarps<T>) * ring) + i / kCaWarps<T> * GT; };
   auto partial = [&](int i) { return p.partials + static_cast<int64_t>(i == 0 ? first : rest + 2 * i) * kCaPartial; };
-  for (int g = warp; g < heads; g += kCaWarps) {
+  for (int g = warp; g < heads; g += kCaWarps<T>) {
     float m = -INFINITY;
     for (int i = lane; i <= more; i += 32) {
       const float mi = __ldcg(partial(i) + GT * D + g);
-      factors[i * GT + g] = mi;
+      factor(i)[g] = mi;
       m = fmaxf(m, mi);
     }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
     float z = 0.f;
     for (int i = lane; i <= more; i += 32) {
-      const float f = ca_factor(factors[i * GT + g], m);
-      factors[i * GT + g] = f;
+      const float f = ca_factor(factor(i)[g], m);
+      factor(i)[g] = f;
       z = fmaf(__ldcg(partial(i) + GT * D + GT + g), f, z);
     }
 #pragma unroll
@@ -473,7 +490,7 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, float* facto
     }
   }
   __syncthreads();
-  for (int o = threadIdx.x * 4; o < heads * D; o += kCaThreads * 4) {
+  for (int o = threadIdx.x * 4; o < heads * D; o += kCaThreads<T> * 4) {
     const int g = o / D;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i <= more; i += kAhead) {
@@ -484,7 +501,7 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, float* facto
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         if (i + j > more) continue;
-        const float f = factors[(i + j) * GT + g];
+        const float f = factor(i + j)[g];
         a.x = fmaf(x[j].x, f, a.x);
         a.y = fmaf(x[j].y, f, a.y);
         a.z = fmaf(x[j].z, f, a.z);
@@ -539,22 +556,24 @@ struct CaPlan {
     per_seq = units_per_seq;
     done = false;
     parts_of = 0;
-    const int lane = threadIdx.x & 31, ctas = gridDim.x;
-    const int64_t units = static_cast<int64_t>(batch) * per_seq, tiles = static_cast<int64_t>(off[batch]) * per_seq;
-    if (units <= ctas) {
-      auto parts = [&](int64_t most) {
+    const int lane = threadIdx.x & 31;
+    const unsigned ctas = gridDim.x;
+    const int64_t all = static_cast<int64_t>(off[batch]) * per_seq;
+    if (static_cast<int64_t>(batch) * per_seq <= ctas && all < (1 << 30)) {
+      const unsigned units = batch * per_seq, tiles = static_cast<unsigned>(all);
+      auto parts = [&](unsigned most) {
         unsigned sum = 0;
-        for (int s = lane; s < batch; s += 32) sum += static_cast<unsigned>((off[s + 1] - off[s] + most - 1) / most);
-        return static_cast<int64_t>(__reduce_add_sync(0xffffffffu, sum)) * per_seq;
+        for (int s = lane; s < batch; s += 32) sum += (off[s + 1] - off[s] + most - 1) / most;
+        return __reduce_add_sync(0xffffffffu, sum) * per_seq;
       };
-      int64_t lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
+      unsigned lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
       hi = max(lo, hi);                    // parts of hi tiles fit: there are fewer than tiles / hi + units of them
       while (lo < hi) {
-        const int64_t mid = (lo + hi) / 2;
+        const unsigned mid = (lo + hi) / 2;
         if (parts(mid) <= ctas) hi = mid;
         else lo = mid + 1;
       }
-      if (hi * ctas <= tiles + static_cast<int64_t>(kCaSpare) * ctas) parts_of = static_cast<int>(hi);
+      if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) parts_of = static_cast<int>(hi);
     }
     if (parts_of) return;
     total = ahead(batch);
@@ -571,7 +590,8 @@ struct CaPlan {
       if (done) return false;
       done = true;
       const int lane = threadIdx.x & 31;
-      int64_t run = 0;                     // parts of the sequences ahead
+      const int cta = static_cast<int>(blockIdx.x);
+      int run = 0;                         // parts of the sequences ahead
       for (int s0 = 0; s0 < batch; s0 += 32) {
         const int x = s0 + lane < batch ? (off[s0 + lane + 1] - off[s0 + lane] + parts_of - 1) / parts_of : 0;
         int sum = x;
@@ -580,19 +600,19 @@ struct CaPlan {
           const int y = __shfl_up_sync(0xffffffffu, sum, o);
           if (lane >= o) sum += y;
         }
-        const unsigned past = __ballot_sync(0xffffffffu, (run + sum) * per_seq > static_cast<int64_t>(blockIdx.x));
+        const unsigned past = __ballot_sync(0xffffffffu, (run + sum) * per_seq > cta);
         if (past) {
           const int l = __ffs(past) - 1, parts = __shfl_sync(0xffffffffu, x, l);
-          const int64_t in_seq = blockIdx.x - (run + __shfl_sync(0xffffffffu, sum, l) - parts) * per_seq;
+          const int in_seq = cta - (run + __shfl_sync(0xffffffffu, sum, l) - parts) * per_seq;
           s->b = s0 + l;
           const int tiles = off[s->b + 1] - off[s->b];
-          s->unit = static_cast<int>(in_seq / parts);
-          const int k = static_cast<int>(in_seq) - s->unit * parts;
+          s->unit = in_seq / parts;
+          const int k = in_seq - s->unit * parts;
           s->tile0 = static_cast<int>(static_cast<int64_t>(tiles) * k / parts);
           s->tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (k + 1) / parts);
           s->whole = parts == 1;
-          s->slot = 2 * blockIdx.x;
-          s->first = s->rest = 2 * (blockIdx.x - k);
+          s->slot = 2 * cta;
+          s->first = s->rest = 2 * (cta - k);
           s->more = parts - 1;
           return true;
         }
@@ -628,18 +648,20 @@ struct CaPlan {
   }
 };
 
-// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory kCaWarps rings (+ 2 GT * D floats in fp32).
+// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory: a ring per warp (+ twice GT * (D + 4)
+// floats in fp32).
 template <typename T, int D, int GT, bool POS>
-__global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
+__global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
   using W = CaWarp<T, D, GT, POS>;
   using Sums = CaSums<T, D, GT, POS>;
   constexpr uint32_t kSlot = 2 * W::TILE;
+  constexpr int WARPS = kCaWarps<T>, THREADS = kCaThreads<T>;
   static_assert(GT * W::HEAD * 4 <= kSlot, "a warp's sums fit the last slot of its ring");
+  static_assert((kCaMaxGrid + WARPS - 1) / WARPS * GT * 4 <= kSlot, "and the factors of a join all warps' last slots");
   extern __shared__ __align__(128) uint8_t ca_smem[];
   __shared__ int32_t s_off[PKV_MAX_CACHE_BATCH + 1];             // tiles of a unit of the sequences ahead
-  __shared__ int32_t s_scan[kCaWarps];
-  __shared__ float s_m[kCaWarps][GT], s_z[kCaWarps][GT];
-  __shared__ float s_factors[kCaMaxGrid * GT];
+  __shared__ int32_t s_scan[WARPS];
+  __shared__ float s_m[WARPS][GT], s_z[WARPS][GT];
   __shared__ int32_t s_last;
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -647,34 +669,37 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
   pdl_wait();
 
   // ---- tiles of every sequence and their running sum
-  {
-    constexpr int PER = PKV_MAX_CACHE_BATCH / kCaThreads;
-    int mine[PER], sum = 0;
-    const int per = (p.batch + kCaThreads - 1) / kCaThreads;     // consecutive sequences of a thread
+  auto tiles_of = [&](int b) { return max(1, (min(max(__ldg(p.lens + b), 0), most) + kCaTile - 1) / kCaTile); };
+  if (p.batch <= 32) {                     // every warp for itself: all write the same
+    const int x = lane < p.batch ? tiles_of(lane) : 0;
+    int run = x;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = tid * per + i;
-      mine[i] = 0;
-      if (i < per && b < p.batch) mine[i] = max(1, (min(max(__ldg(p.lens + b), 0), most) + kCaTile - 1) / kCaTile);
-      sum += mine[i];
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += y;
     }
+    if (lane < p.batch) s_off[lane + 1] = run;
+    if (lane == 0) s_off[0] = 0;
+    __syncwarp();
+  } else {
+    const int per = (p.batch + THREADS - 1) / THREADS;           // consecutive sequences of a thread
+    int sum = 0;
+    for (int i = 0, b = tid * per; i < per && b < p.batch; ++i, ++b) sum += tiles_of(b);
     int run = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, run, o);
-      if (lane >= o) run += x;
+      const int y = __shfl_up_sync(0xffffffffu, run, o);
+      if (lane >= o) run += y;
     }
     if (lane == 31) s_scan[warp] = run;
     __syncthreads();
     for (int w = 0; w < warp; ++w) run += s_scan[w];
     run -= sum;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int b = tid * per + i;
-      if (i < per && b < p.batch) s_off[b] = run;
-      run += mine[i];
+    for (int i = 0, b = tid * per; i < per && b < p.batch; ++i, ++b) {
+      s_off[b] = run;
+      run += tiles_of(b);
     }
-    if (tid == kCaThreads - 1) s_off[p.batch] = run;
+    if (tid == THREADS - 1) s_off[p.batch] = run;
     __syncthreads();
   }
   CaPlan plan;
@@ -689,10 +714,18 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
   const T* q0;
   int first, heads, hq;
   uint32_t seen[kCaStages], far[kCaStages];                      // of the tiles in the ring, oldest first
-  int64_t mine_last;                                             // where the rows of the last slot's tile lie
+  int64_t mine_last, next;                                       // where the rows of the last slot's tile lie, and the next one's
+  int next_pos;
   int q_buffer = 0;
   Sums sums;
-  auto look_up = [&](int t0, uint32_t* f) { return ca_look_up<POS>(p, rows, t0 + (lane & 15), lane < 16, f); };
+  // Rows are looked up in two steps, a tile apart: a row's place, then its position.  Lane l has row l % TR.
+  auto place = [&](int t0) { return ca_place<POS>(p, rows, t0 + lane % W::TR, lane < W::TR); };
+  auto position = [&](int64_t at) { return POS && at >= 0 ? __ldg(p.pos_pool + at) : 0; };
+  auto judge = [&](int64_t at, int pos, uint32_t* f) -> int64_t {                  // the place, -1 if the row is not seen
+    *f = 0;
+    return POS && at >= 0 && !ca_seen<POS>(p, rows, pos, f) ? -1 : at;
+  };
+  constexpr uint32_t kRowBits = W::TR == 32 ? 0xffffffffu : (1u << W::TR) - 1u;
   auto copy_in = [&](uint32_t slot, uint32_t there, int64_t mine) {
     if (there) W::copy_tile(p, ring + slot, mine);
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -706,20 +739,27 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
     rows.table = p.table + (static_cast<int64_t>(seg.b) * p.num_kv_heads + h) * p.max_pages;
     rows.rows = min(min(max(__ldg(p.lens + seg.b), 0), most), seg.tile1 * kCaTile);
     rows.q_pos = POS ? __ldg(p.q_pos + seg.b) : 0;
-    first = seg.tile0 * kCaTile + warp * 16;
+    first = seg.tile0 * kCaTile + warp * W::TR;
     int64_t mine[kCaStages];
+    int pos[kCaStages];
 #pragma unroll
-    for (int s = 0; s < kCaStages; ++s) mine[s] = look_up(first + s * kCaTile, &far[s]);
+    for (int s = 0; s < kCaStages; ++s) mine[s] = place(first + s * kCaTile);
+    next = place(first + kCaStages * kCaTile);
+#pragma unroll
+    for (int s = 0; s < kCaStages; ++s) pos[s] = position(mine[s]);
+    next_pos = position(next);
 #pragma unroll
     for (int s = 0; s < kCaStages; ++s) {
-      seen[s] = __ballot_sync(0xffffffffu, mine[s] >= 0);
+      mine[s] = judge(mine[s], pos[s], &far[s]);
+      seen[s] = __ballot_sync(0xffffffffu, mine[s] >= 0) & kRowBits;
       if (s < kCaStages - 1) copy_in(s * kSlot, seen[s], mine[s]);
     }
     mine_last = mine[kCaStages - 1];
     if constexpr (sizeof(T) == 4) {
-      float* q_shared = reinterpret_cast<float*>(ca_smem + kCaWarps * W::kRing) + q_buffer * (GT * D);
+      float* q_shared = reinterpret_cast<float*>(ca_smem + WARPS * W::kRing) + q_buffer * (GT * (D + 4));
       q_buffer ^= 1;
-      for (int i = tid; i < GT * D; i += kCaThreads) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
+      for (int i = tid; i < GT * D; i += THREADS) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
+      if (POS && tid < GT) q_shared[GT * D + tid] = p.slopes && tid < heads ? __ldg(p.slopes + hq + tid) * 1.4426950408889634f : 0.f;
       sums.start(p, q_shared, heads, hq);
     } else {
       sums.start(p, q0, heads, hq);
@@ -729,8 +769,7 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
   while (true) {
     if constexpr (sizeof(T) == 4) __syncthreads();               // the queries are there
     copy_in(kAcc, seen[kCaStages - 1], mine_last);
-    uint32_t far_next;
-    int64_t next = look_up(first + kCaStages * kCaTile, &far_next);
+    int64_t second = place(first + (kCaStages + 1) * kCaTile);   // one tile further
 
     // ---- the warp's rows
     uint32_t slot = 0;
@@ -744,10 +783,12 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
         seen[s] = seen[s + 1];
         far[s] = far[s + 1];
       }
-      seen[kCaStages - 1] = __ballot_sync(0xffffffffu, next >= 0);
-      far[kCaStages - 1] = far_next;
-      copy_in(slot, seen[kCaStages - 1], next);
-      next = look_up(t0 + (kCaStages + 1) * kCaTile, &far_next);
+      const int64_t mine = judge(next, next_pos, &far[kCaStages - 1]);
+      seen[kCaStages - 1] = __ballot_sync(0xffffffffu, mine >= 0) & kRowBits;
+      copy_in(slot, seen[kCaStages - 1], mine);
+      next = second;
+      next_pos = position(next);
+      second = place(t0 + (kCaStages + 2) * kCaTile);
       slot = slot == kAcc ? 0 : slot + kSlot;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -763,14 +804,14 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
     __syncthreads();
     // the output, or a partial result that the unit's last CTA joins with the others
     float* part = p.partials + static_cast<int64_t>(was.slot) * kCaPartial;
-    for (int o = tid; o < heads_was * D; o += kCaThreads) {
+    for (int o = tid; o < heads_was * D; o += THREADS) {
       const int g = o / D, channel = o - g * D;
       float m = s_m[0][g];
 #pragma unroll
-      for (int w = 1; w < kCaWarps; ++w) m = fmaxf(m, s_m[w][g]);
+      for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w][g]);
       float z = 0.f, a = 0.f;
 #pragma unroll
-      for (int w = 0; w < kCaWarps; ++w) {
+      for (int w = 0; w < WARPS; ++w) {
         const float f = ca_factor(s_m[w][g], m);
         z = fmaf(s_z[w][g], f, z);
         a = fmaf(reinterpret_cast<const float*>(ca_smem + w * W::kRing + kAcc)[g * W::HEAD + channel], f, a);
@@ -795,7 +836,7 @@ __global__ void __launch_bounds__(kCaThreads) cache_attend_kernel(const __grid_c
         __threadfence();
       }
       __syncthreads();
-      if (s_last) ca_join<D, GT>(p, s_factors, was.first, was.more, was.rest, heads_was, head0);
+      if (s_last) ca_join<T, D, GT>(p, ca_smem + kAcc, static_cast<uint32_t>(W::kRing), was.first, was.more, was.rest, heads_was, head0);
     }
     if (!have) return;
     __syncthreads();                       // the sums have been read: the last slot may be filled
