@@ -156,9 +156,9 @@ int launch_rotary(const pkv_config* c, const pkv_rotary* plan, int inverse, Rota
 bool tokens_ok(int64_t batch, int64_t tokens) { return batch >= 1 && tokens >= 1 && batch * tokens <= INT32_MAX; }
 
 // ---------------------------------------------------------------- attention
-template <typename T, int D, int GT, bool POS>
+template <typename T, int D, int GT, int POS>
 int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st) {
-  constexpr size_t kSmem = kCaWarps<T> * CaWarp<T, D, GT, POS>::kRing + (sizeof(T) == 4 ? 2 * GT * (D + 4) * 4 : 0);
+  constexpr size_t kSmem = kCaWarps<T> * CaWarp<T, D, GT, POS>::kRing + 2 * GT * (sizeof(T) == 4 ? (D + 4) * 4 : D * 2 + 64);
   static std::atomic<int> per_sm[64];      // CTAs that an SM holds, once the kernel's shared memory is set up on a device
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return PKV_ERR_CUDA;
@@ -171,18 +171,22 @@ int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st)
   }
   const int sms = device_sm_count();
   if (sms <= 0) return PKV_ERR_CUDA;
+  const int64_t units = static_cast<int64_t>(p.batch) * p.num_kv_heads * p.head_blocks;
+  if (units <= 2 * sms) fit = std::min(fit, 2);                  // (see kCaPerSm)
   // no more CTAs than there can be tiles
-  const int64_t tiles = (max_rows + kCaTile - 1) / kCaTile * p.batch * p.num_kv_heads * p.head_blocks;
-  const int grid = static_cast<int>(std::min<int64_t>(std::min(kCaMaxGrid, sms * fit), tiles));
+  const int grid = static_cast<int>(std::min<int64_t>(std::min(kCaMaxGrid, sms * fit), (max_rows + kCaTile - 1) / kCaTile * units));
   launch_pdl(cache_attend_kernel<T, D, GT, POS>, dim3(grid), dim3(kCaThreads<T>), kSmem, st, p);
   return check_launch();
 }
 
 template <typename T, int D>
-int dispatch_cache_attend(CacheAttendParams& p, int gt, bool pos, int64_t max_rows, cudaStream_t st) {
+int dispatch_cache_attend(CacheAttendParams& p, int gt, int64_t max_rows, cudaStream_t st) {
+  const int pos = !p.q_pos ? 0 : (p.slopes ? 2 : 1);
   if (gt == 4)
-    return pos ? launch_cache_attend<T, D, 4, true>(p, max_rows, st) : launch_cache_attend<T, D, 4, false>(p, max_rows, st);
-  return pos ? launch_cache_attend<T, D, 8, true>(p, max_rows, st) : launch_cache_attend<T, D, 8, false>(p, max_rows, st);
+    return pos == 0 ? launch_cache_attend<T, D, 4, 0>(p, max_rows, st)
+                    : (pos == 1 ? launch_cache_attend<T, D, 4, 1>(p, max_rows, st) : launch_cache_attend<T, D, 4, 2>(p, max_rows, st));
+  return pos == 0 ? launch_cache_attend<T, D, 8, 0>(p, max_rows, st)
+                  : (pos == 1 ? launch_cache_attend<T, D, 8, 1>(p, max_rows, st) : launch_cache_attend<T, D, 8, 2>(p, max_rows, st));
 }
 
 // ---------------------------------------------------------------- pages
@@ -438,14 +442,14 @@ int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cac
   p.cap_log2 = static_cast<float>(o.softcap * log2e);
   p.scale_log2 = static_cast<float>(o.softcap > 0.f ? scale / o.softcap : scale * log2e);
   const int gt = heads_per_cta(cfg);
-  const bool pos = o.q_positions != nullptr, wide = cfg->head_dim == 128;
+  const bool wide = cfg->head_dim == 128;
   const int64_t rows = static_cast<int64_t>(cache->max_pages) * cache->page_size;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (cfg->dtype) {
-    case PKV_DTYPE_FP32: return wide ? dispatch_cache_attend<float, 128>(p, gt, pos, rows, st) : dispatch_cache_attend<float, 64>(p, gt, pos, rows, st);
-    case PKV_DTYPE_FP16: return wide ? dispatch_cache_attend<__half, 128>(p, gt, pos, rows, st) : dispatch_cache_attend<__half, 64>(p, gt, pos, rows, st);
+    case PKV_DTYPE_FP32: return wide ? dispatch_cache_attend<float, 128>(p, gt, rows, st) : dispatch_cache_attend<float, 64>(p, gt, rows, st);
+    case PKV_DTYPE_FP16: return wide ? dispatch_cache_attend<__half, 128>(p, gt, rows, st) : dispatch_cache_attend<__half, 64>(p, gt, rows, st);
     default:
-      return wide ? dispatch_cache_attend<__nv_bfloat16, 128>(p, gt, pos, rows, st) : dispatch_cache_attend<__nv_bfloat16, 64>(p, gt, pos, rows, st);
+      return wide ? dispatch_cache_attend<__nv_bfloat16, 128>(p, gt, rows, st) : dispatch_cache_attend<__nv_bfloat16, 64>(p, gt, rows, st);
   }
 }
 

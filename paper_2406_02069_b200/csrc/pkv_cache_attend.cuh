@@ -25,7 +25,7 @@
 namespace pkv {
 
 constexpr int kCaTile = 64;                // rows of a tile, shared by the warps of a CTA
-constexpr int kCaStages = 3;               // a warp's tiles in shared memory or on their way
+constexpr int kCaStages = 2;               // a warp's tiles in shared memory or on their way
 // Warps of a CTA: four with 16 rows each of 16-bit types, eight with 8 rows each in fp32, where a row takes twice the bytes and
 // several times the instructions.
 template <typename T>
@@ -34,11 +34,15 @@ template <typename T>
 constexpr int kCaThreads = kCaWarps<T> * 32;
 template <typename T>
 constexpr int kCaRows = kCaTile / kCaWarps<T>;
-constexpr int kCaMaxGrid = 2 * 160;        // CTAs at most (sizes the partial sums in the workspace)
+// CTAs to an SM: three where there is a unit for each, two where units are split anyway and more parts only mean more to join
+// (131072 rows x 8 KV heads x 8 query heads: two 98 us, three 106; 64 sequences of 129 to 4096 rows, capped, window: 123 and 106).
+constexpr int kCaPerSm = 3;
+constexpr int kCaMaxGrid = kCaPerSm * 160; // CTAs at most (sizes the partial sums in the workspace)
 constexpr int kCaMaxHeads = 8;             // query heads of a CTA at most
 // Floats of one partial result: sums, then exponents, then weights' sums.
 constexpr int kCaPartial = kCaMaxHeads * (128 + 2);
 
+// POS of the templates: 0 positions play no part, 1 they say which rows are seen, 2 and give a bias.
 struct CacheAttendParams {
   const void* q;
   int64_t q_sb, q_sh;
@@ -63,14 +67,15 @@ struct CacheAttendParams {
 };
 
 // Logit in powers of two from a dot product; far: p - p_r where there is a bias.
+template <int POS>
 __device__ __forceinline__ float ca_logit(const CacheAttendParams& p, float dot, float slope_log2, float far) {
   float x = dot * p.scale_log2;
   if (p.cap_log2 != 0.f) x = p.cap_log2 * tanhf(x);
-  return fmaf(-slope_log2, far, x);
+  return POS == 2 ? fmaf(-slope_log2, far, x) : x;
 }
 
 // The rows of one KV head of one sequence, as a warp looks them up.
-template <bool POS>
+template <int POS>
 struct CaRows {
   const int32_t* table;
   int32_t rows;                            // that the segment goes up to
@@ -78,7 +83,7 @@ struct CaRows {
 };
 
 // Row r's place in the pool, counted in rows; -1 if it has none.
-template <bool POS>
+template <int POS>
 __device__ __forceinline__ int64_t ca_place(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report) {
   if (r >= s.rows) return -1;
   const int j = p.page_shift >= 0 ? r >> p.page_shift : r / p.page_size;
@@ -91,7 +96,7 @@ __device__ __forceinline__ int64_t ca_place(const CacheAttendParams& p, const Ca
 }
 
 // Whether the row at a place is seen, by its position; *far: p - p_r.
-template <bool POS>
+template <int POS>
 __device__ __forceinline__ bool ca_seen(const CacheAttendParams& p, const CaRows<POS>& s, int pos, uint32_t* far) {
   *far = static_cast<uint32_t>(s.q_pos) - static_cast<uint32_t>(pos);         // positions may be 2^31 apart and more
   return pos <= s.q_pos && (p.window == 0 || *far < static_cast<uint32_t>(p.window) || pos < p.prefix);
@@ -99,7 +104,7 @@ __device__ __forceinline__ bool ca_seen(const CacheAttendParams& p, const CaRows
 
 // Sums of one query head over the warp's rows on the fp32 pipe, for rows that hold infinities or NaN:
 // in the matrix product every part of a weight meets every value, and a part that is zero or negative makes NaN of an infinity.
-template <typename T, int D, bool POS>
+template <typename T, int D, int POS>
 __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const CaRows<POS>& s, const T* q, int first, float slope, float ref,
                                             float* acc) {
   constexpr int PER = D / 32;
@@ -124,7 +129,7 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
       for (int c = 0; c < PER; ++c) dot = fmaf(qv[c], to_float(k[c]), dot);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-      const float w = exp2f(ca_logit(p, dot, slope, __uint2float_rn(far)) - ref);
+      const float w = exp2f(ca_logit<POS>(p, dot, slope, __uint2float_rn(far)) - ref);
 #pragma unroll
       for (int c = 0; c < PER; ++c) a[c] = fmaf(w, to_float(v[c]), a[c]);
     }
@@ -134,7 +139,7 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
 
 // One warp's sums over rows first .. first + kCaRows - 1, first + kCaTile .. of a segment: weights' sums to z[GT], exponents that they
 // are relative to (-infinity: no seen row) to m[GT], weighted sums of V to acc[GT][D + 4], all in shared memory.
-template <typename T, int D, int GT, bool POS>
+template <typename T, int D, int GT, int POS>
 struct CaWarp {
   static constexpr int TR = kCaRows<T>;                          // rows of the warp's tile
   static constexpr uint32_t ROW = D * sizeof(T), TILE = TR * ROW;
@@ -168,12 +173,14 @@ struct CaWarp {
 };
 
 // State of the sums of a warp, and one step over a tile; 16-bit rows.
-template <typename T, int D, int GT, bool POS>
+template <typename T, int D, int GT, int POS>
 struct CaSums {
   using W = CaWarp<T, D, GT, POS>;
   using X = Dec16<T>;
   static constexpr int KC = D / 32, VC = D / 64;
-  uint4 q[KC];
+  // Queries in shared memory, rows of kQ bytes: eight lanes that read 16 bytes each touch every bank once.
+  static constexpr uint32_t kQ = D * 2 + 64;
+  uint32_t q;
   // [channel octet's element][fragment rows g, g + 8]: channels of two of the octets.  Each tile's products are added to
   // them on the fp32 pipe, which rounds to nearest; the tensor core's own accumulation cuts off, and over 131072 rows that
   // came to 2e-6 of the output (4e-7 this way).
@@ -181,13 +188,11 @@ struct CaSums {
   float m, z;                              // of head g % GT: m over the warp's rows, z over this lane's
   float slope;
 
-  __device__ __forceinline__ void start(const CacheAttendParams& p, const T* q0, int heads, int hq) {
+  __device__ __forceinline__ void start(const CacheAttendParams& p, uint32_t q_shared, int heads, int hq) {
     const int lane = threadIdx.x & 31, g = (lane >> 2) % GT, c = lane & 3;
     const bool there = g < heads;
-#pragma unroll
-    for (int j = 0; j < KC; ++j)
-      q[j] = there ? *reinterpret_cast<const uint4*>(q0 + g * p.q_sh + j * 32 + c * 8) : make_uint4(0, 0, 0, 0);
-    slope = POS && p.slopes && there ? __ldg(p.slopes + hq + g) * 1.4426950408889634f : 0.f;
+    q = q_shared + g * kQ + c * 16;
+    slope = POS == 2 && there ? __ldg(p.slopes + hq + g) * 1.4426950408889634f : 0.f;
 #pragma unroll
     for (int i = 0; i < VC * 8; ++i) o[i][0] = o[i][1] = 0ull;
     m = -INFINITY;
@@ -199,21 +204,29 @@ struct CaSums {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     float x[2][2];
     float mx = -INFINITY;
+    float s0[2][4], s1[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s0[t][e] = s1[t][e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < KC; ++j) {
+      const uint4 qj = dec_lds16(q + j * 64);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint4 k = dec_lds16(k_at + (t * 8 + g) * W::ROW + W::k_place(g, j * 4 + c));
+        X::mma(s0[t], qj.x, qj.x, qj.y, qj.y, k.x, k.y);
+        X::mma(s1[t], qj.z, qj.z, qj.w, qj.w, k.z, k.w);
+      }
+    }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < KC; ++j) {
-        const uint4 k = dec_lds16(k_at + (t * 8 + g) * W::ROW + W::k_place(g, j * 4 + c));
-        X::mma(s0, q[j].x, q[j].x, q[j].y, q[j].y, k.x, k.y);
-        X::mma(s1, q[j].z, q[j].z, q[j].w, q[j].w, k.z, k.w);
-      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = t * 8 + 2 * c + i;
         float d = 0.f;
-        if (POS) d = __uint2float_rn(__shfl_sync(0xffffffffu, far, r));
-        x[t][i] = (seen >> r) & 1u ? ca_logit(p, s0[i] + s1[i], slope, d) : -INFINITY;
+        if (POS == 2) d = __uint2float_rn(__shfl_sync(0xffffffffu, far, r));
+        x[t][i] = (seen >> r) & 1u ? ca_logit<POS>(p, s0[t][i] + s1[t][i], slope, d) : -INFINITY;
         mx = fmaxf(mx, x[t][i]);
       }
     }
@@ -343,7 +356,7 @@ struct CaSums {
 
 // fp32 rows.  Lane l has channels of quarter l / 8 of row l % 8 for the dot products, and channels 4 (l % PIECES) .. of the rows of
 // parity l / PIECES (all rows where a row has 32 pieces) for the weighted sums.
-template <int D, int GT, bool POS>
+template <int D, int GT, int POS>
 struct CaSums<float, D, GT, POS> {
   using W = CaWarp<float, D, GT, POS>;
   static constexpr int PIECES = W::PIECES, VR = W::ROWS_AT_ONCE;
@@ -381,7 +394,7 @@ struct CaSums<float, D, GT, POS> {
       }
     }
     const bool live = (seen >> row) & 1u;
-    const float d = POS ? __uint2float_rn(far) : 0.f;             // lane l has row l % 8's
+    const float d = POS == 2 ? __uint2float_rn(far) : 0.f;        // lane l has row l % 8's
     float w[GT];
 #pragma unroll
     for (int g = 0; g < GT; ++g) {
@@ -390,8 +403,8 @@ struct CaSums<float, D, GT, POS> {
       float dot = a + b;
       dot += __shfl_xor_sync(0xffffffffu, dot, 8);
       dot += __shfl_xor_sync(0xffffffffu, dot, 16);
-      const float slope = POS ? q0[GT * D + g] : 0.f;             // (behind the queries)
-      const float x = live ? ca_logit(p, dot, slope, d) : -INFINITY;
+      const float slope = POS == 2 ? q0[GT * D + g] : 0.f;        // (behind the queries)
+      const float x = live ? ca_logit<POS>(p, dot, slope, d) : -INFINITY;
       float mx = x;
 #pragma unroll
       for (int s = 4; s > 0; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
@@ -467,10 +480,17 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   auto factor = [&](int i) -> float* { return reinterpret_cast<float*>(last_slots + (i % kCaWarps<T>) * ring) + i / kCaWarps<T> * GT; };
   auto partial = [&](int i) { return p.partials + static_cast<int64_t>(i == 0 ? first : rest + 2 * i) * kCaPartial; };
+  float4 x[kAhead];
+  auto fetch = [&](int i, int o) {         // (the last one again behind it: loads without a condition go out together)
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) x[j] = __ldcg(reinterpret_cast<const float4*>(partial(min(i + j, more)) + o));
+  };
+  fetch(0, min(static_cast<int>(threadIdx.x) * 4, heads * D - 4));               // on their way while the factors are found
   for (int g = warp; g < heads; g += kCaWarps<T>) {
-    float m = -INFINITY;
+    float m = -INFINITY, z0 = 0.f;
     for (int i = lane; i <= more; i += 32) {
       const float mi = __ldcg(partial(i) + GT * D + g);
+      if (i == lane) z0 = __ldcg(partial(i) + GT * D + GT + g);
       factor(i)[g] = mi;
       m = fmaxf(m, mi);
     }
@@ -480,7 +500,7 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
     for (int i = lane; i <= more; i += 32) {
       const float f = ca_factor(factor(i)[g], m);
       factor(i)[g] = f;
-      z = fmaf(__ldcg(partial(i) + GT * D + GT + g), f, z);
+      z = fmaf(i == lane ? z0 : __ldcg(partial(i) + GT * D + GT + g), f, z);
     }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) z += __shfl_xor_sync(0xffffffffu, z, s);
@@ -494,18 +514,16 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
     const int g = o / D;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i <= more; i += kAhead) {
-      float4 x[kAhead];
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j)
-        if (i + j <= more) x[j] = __ldcg(reinterpret_cast<const float4*>(partial(i + j) + o));
+      if (i > 0 || o >= kCaThreads<T> * 4) fetch(i, o);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (i + j > more) continue;
-        const float f = factor(i + j)[g];
-        a.x = fmaf(x[j].x, f, a.x);
-        a.y = fmaf(x[j].y, f, a.y);
-        a.z = fmaf(x[j].z, f, a.z);
-        a.w = fmaf(x[j].w, f, a.w);
+        if (i + j <= more) {
+          const float f = factor(i + j)[g];
+          a.x = fmaf(x[j].x, f, a.x);
+          a.y = fmaf(x[j].y, f, a.y);
+          a.z = fmaf(x[j].z, f, a.z);
+          a.w = fmaf(x[j].w, f, a.w);
+        }
       }
     }
     const float m = s_jm[g], z = s_jz[g];
@@ -529,129 +547,136 @@ constexpr int kCaStart = 2;
 constexpr int kCaSpare = 3;                // tiles that parts may have more than equal ranges would
 
 struct CaSegment {
-  int b, unit;                             // unit of the sequence: KV head * head_blocks + block
+  int b, unit;                             // sequence (-1: no segment) and unit of it: KV head * head_blocks + block
   int tile0, tile1;
   bool whole;                              // the unit's only segment
   int slot;                                // where this segment's partial result goes
   int first, rest, more;                   // where the unit's are: the first one, and rest + 2 .. rest + 2 more
 };
 
+// Lies in shared memory: one thread works it out while the others are at the sums.
 struct CaPlan {
-  const int32_t* off;
-  int batch, per_seq;                      // units of a sequence
-  int64_t begin, end, total;               // this CTA's range, and all of it (equal ranges)
-  int64_t at;
+  int batch, per_seq;                      // sequences, units of each
   int b;
-  int parts_of;                            // > 0: parts of at most so many tiles
-  bool done;
+  int64_t begin, end, total;               // this CTA's range, and all of it
+  int64_t at;                              // of the next segment; end with parts
 
   __device__ __forceinline__ int64_t start_of(int64_t cta) const { return total * cta / gridDim.x; }
   __device__ __forceinline__ int64_t owner(int64_t tile) const { return ((tile + 1) * gridDim.x - 1) / total; }
-  __device__ __forceinline__ int64_t ahead(int s) const { return static_cast<int64_t>(off[s] + kCaStart * s) * per_seq; }
-
-  // All warps come to the same plan.
-  __device__ __forceinline__ void make(const int32_t* s_off, int sequences, int units_per_seq) {
-    off = s_off;
-    batch = sequences;
-    per_seq = units_per_seq;
-    done = false;
-    parts_of = 0;
-    const int lane = threadIdx.x & 31;
-    const unsigned ctas = gridDim.x;
-    const int64_t all = static_cast<int64_t>(off[batch]) * per_seq;
-    if (static_cast<int64_t>(batch) * per_seq <= ctas && all < (1 << 30)) {
-      const unsigned units = batch * per_seq, tiles = static_cast<unsigned>(all);
-      auto parts = [&](unsigned most) {
-        unsigned sum = 0;
-        for (int s = lane; s < batch; s += 32) sum += (off[s + 1] - off[s] + most - 1) / most;
-        return __reduce_add_sync(0xffffffffu, sum) * per_seq;
-      };
-      unsigned lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
-      hi = max(lo, hi);                    // parts of hi tiles fit: there are fewer than tiles / hi + units of them
-      while (lo < hi) {
-        const unsigned mid = (lo + hi) / 2;
-        if (parts(mid) <= ctas) hi = mid;
-        else lo = mid + 1;
-      }
-      if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) parts_of = static_cast<int>(hi);
-    }
-    if (parts_of) return;
-    total = ahead(batch);
-    at = begin = start_of(blockIdx.x);
-    end = start_of(blockIdx.x + 1);
-    b = 0;
-    for (int step = 512; step > 0; step >>= 1)                   // the last sequence that starts at or before `at`
-      if (b + step < batch && ahead(b + step) <= at) b += step;
-  }
-
-  // The next segment of this CTA, false behind the last one.
-  __device__ __forceinline__ bool next(CaSegment* s) {
-    if (parts_of) {
-      if (done) return false;
-      done = true;
-      const int lane = threadIdx.x & 31;
-      const int cta = static_cast<int>(blockIdx.x);
-      int run = 0;                         // parts of the sequences ahead
-      for (int s0 = 0; s0 < batch; s0 += 32) {
-        const int x = s0 + lane < batch ? (off[s0 + lane + 1] - off[s0 + lane] + parts_of - 1) / parts_of : 0;
-        int sum = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int y = __shfl_up_sync(0xffffffffu, sum, o);
-          if (lane >= o) sum += y;
-        }
-        const unsigned past = __ballot_sync(0xffffffffu, (run + sum) * per_seq > cta);
-        if (past) {
-          const int l = __ffs(past) - 1, parts = __shfl_sync(0xffffffffu, x, l);
-          const int in_seq = cta - (run + __shfl_sync(0xffffffffu, sum, l) - parts) * per_seq;
-          s->b = s0 + l;
-          const int tiles = off[s->b + 1] - off[s->b];
-          s->unit = in_seq / parts;
-          const int k = in_seq - s->unit * parts;
-          s->tile0 = static_cast<int>(static_cast<int64_t>(tiles) * k / parts);
-          s->tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (k + 1) / parts);
-          s->whole = parts == 1;
-          s->slot = 2 * cta;
-          s->first = s->rest = 2 * (cta - k);
-          s->more = parts - 1;
-          return true;
-        }
-        run += __shfl_sync(0xffffffffu, sum, 31);
-      }
-      return false;                        // more CTAs than parts
-    }
-    while (at < end) {
-      while (at >= ahead(b + 1)) ++b;
-      const int tiles = off[b + 1] - off[b], counted = tiles + kCaStart;
-      const int64_t in_seq = at - ahead(b);
-      s->b = b;
-      s->unit = static_cast<int>(in_seq / counted);
-      const int v0 = static_cast<int>(in_seq - static_cast<int64_t>(s->unit) * counted);
-      const int v1 = static_cast<int>(min(static_cast<int64_t>(counted), v0 + (end - at)));
-      const int64_t unit0 = at - v0;
-      at += v1 - v0;
-      s->tile0 = max(0, v0 - kCaStart);
-      s->tile1 = max(0, v1 - kCaStart);
-      if (s->tile0 == s->tile1) continue;
-      s->whole = s->tile0 == 0 && s->tile1 == tiles;
-      if (!s->whole) {
-        // a CTA has at most one unit that it did not start (place 0) and one that it does not finish (place 1)
-        const int64_t c0 = owner(unit0 + kCaStart);
-        s->more = static_cast<int>(owner(unit0 + counted - 1) - c0);
-        s->slot = 2 * blockIdx.x + (begin <= unit0 ? 1 : 0);
-        s->rest = static_cast<int>(2 * c0);
-        s->first = s->rest + (start_of(c0) <= unit0 ? 1 : 0);
-      }
-      return true;
-    }
-    return false;
-  }
+  __device__ __forceinline__ int64_t ahead(const int32_t* off, int s) const { return static_cast<int64_t>(off[s] + kCaStart * s) * per_seq; }
 };
+
+// The next segment of this CTA's range.  One thread.
+__device__ __noinline__ void ca_next(const int32_t* off, CaPlan* plan, CaSegment* s) {
+  CaPlan p = *plan;
+  s->b = -1;
+  while (p.at < p.end) {
+    while (p.at >= p.ahead(off, p.b + 1)) ++p.b;
+    const int tiles = off[p.b + 1] - off[p.b], counted = tiles + kCaStart;
+    const int64_t in_seq = p.at - p.ahead(off, p.b);
+    const int unit = static_cast<int>(in_seq / counted);
+    const int v0 = static_cast<int>(in_seq - static_cast<int64_t>(unit) * counted);
+    const int v1 = static_cast<int>(min(static_cast<int64_t>(counted), v0 + (p.end - p.at)));
+    const int64_t unit0 = p.at - v0;
+    p.at += v1 - v0;
+    const int tile0 = max(0, v0 - kCaStart), tile1 = max(0, v1 - kCaStart);
+    if (tile0 == tile1) continue;
+    s->b = p.b;
+    s->unit = unit;
+    s->tile0 = tile0;
+    s->tile1 = tile1;
+    s->whole = tile0 == 0 && tile1 == tiles;
+    if (!s->whole) {
+      // a CTA has at most one unit that it did not start (place 0) and one that it does not finish (place 1)
+      const int64_t c0 = p.owner(unit0 + kCaStart);
+      s->more = static_cast<int>(p.owner(unit0 + counted - 1) - c0);
+      s->slot = 2 * blockIdx.x + (p.begin <= unit0 ? 1 : 0);
+      s->rest = static_cast<int>(2 * c0);
+      s->first = s->rest + (p.start_of(c0) <= unit0 ? 1 : 0);
+    }
+    break;
+  }
+  plan->at = p.at;
+  plan->b = p.b;
+}
+
+// The plan of a call and this CTA's first two segments.  One warp.
+__device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq, CaPlan* plan, CaSegment* seg) {
+  const int lane = threadIdx.x & 31;
+  const unsigned ctas = gridDim.x;
+  const int64_t all = static_cast<int64_t>(off[batch]) * per_seq;
+  if (lane == 0) {
+    seg[0].b = seg[1].b = -1;
+    plan->batch = batch;
+    plan->per_seq = per_seq;
+    plan->at = plan->end = 0;
+    plan->b = 0;
+  }
+  int most = 0;                            // tiles of a part, 0: equal ranges
+  if (static_cast<int64_t>(batch) * per_seq <= ctas && all < (1 << 30)) {
+    const unsigned units = batch * per_seq, tiles = static_cast<unsigned>(all);
+    auto parts = [&](unsigned most) {
+      unsigned sum = 0;
+      for (int s = lane; s < batch; s += 32) sum += (off[s + 1] - off[s] + most - 1) / most;
+      return __reduce_add_sync(0xffffffffu, sum) * per_seq;
+    };
+    unsigned lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
+    hi = max(lo, hi);                      // parts of hi tiles fit: there are fewer than tiles / hi + units of them
+    while (lo < hi) {
+      const unsigned mid = (lo + hi) / 2;
+      if (parts(mid) <= ctas) hi = mid;
+      else lo = mid + 1;
+    }
+    if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) most = static_cast<int>(hi);
+  }
+  __syncwarp();
+  if (most == 0) {
+    if (lane) return;
+    plan->total = plan->ahead(off, batch);
+    plan->at = plan->begin = plan->start_of(blockIdx.x);
+    plan->end = plan->start_of(blockIdx.x + 1);
+    int b = 0;
+    for (int step = PKV_MAX_CACHE_BATCH / 2; step > 0; step >>= 1)   // the last sequence that starts at or before `at`
+      if (b + step < batch && plan->ahead(off, b + step) <= plan->at) b += step;
+    plan->b = b;
+    ca_next(off, plan, &seg[0]);
+    ca_next(off, plan, &seg[1]);
+    return;
+  }
+  const int cta = static_cast<int>(blockIdx.x);
+  int run = 0;                             // parts of the sequences ahead
+  for (int s0 = 0; s0 < batch; s0 += 32) {
+    const int x = s0 + lane < batch ? (off[s0 + lane + 1] - off[s0 + lane] + most - 1) / most : 0;
+    int sum = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += y;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, (run + sum) * per_seq > cta);
+    if (past) {
+      if (lane == __ffs(past) - 1) {
+        const int b = s0 + lane, tiles = off[b + 1] - off[b], in_seq = cta - (run + sum - x) * per_seq;
+        const int unit = in_seq / x, k = in_seq - unit * x;
+        seg[0].b = b;
+        seg[0].unit = unit;
+        seg[0].tile0 = static_cast<int>(static_cast<int64_t>(tiles) * k / x);
+        seg[0].tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (k + 1) / x);
+        seg[0].whole = x == 1;
+        seg[0].slot = 2 * cta;
+        seg[0].first = seg[0].rest = 2 * (cta - k);
+        seg[0].more = x - 1;
+      }
+      return;
+    }
+    run += __shfl_sync(0xffffffffu, sum, 31);
+  }
+}
 
 // grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory: a ring per warp (+ twice GT * (D + 4)
 // floats in fp32).
-template <typename T, int D, int GT, bool POS>
-__global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
+template <typename T, int D, int GT, int POS>
+__global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
   using W = CaWarp<T, D, GT, POS>;
   using Sums = CaSums<T, D, GT, POS>;
   constexpr uint32_t kSlot = 2 * W::TILE;
@@ -663,6 +688,8 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
   __shared__ int32_t s_scan[WARPS];
   __shared__ float s_m[WARPS][GT], s_z[WARPS][GT];
   __shared__ int32_t s_last;
+  __shared__ CaPlan s_plan;
+  __shared__ CaSegment s_seg[3];         // the segment that is worked on, the next one and the one after it, in turn
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int most = static_cast<int>(static_cast<int64_t>(p.max_pages) * p.page_size);      // the host keeps it below 2^30
@@ -702,17 +729,15 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
     if (tid == THREADS - 1) s_off[p.batch] = run;
     __syncthreads();
   }
-  CaPlan plan;
-  plan.make(s_off, p.batch, p.num_kv_heads * p.head_blocks);
-  CaSegment seg;
-  bool have = plan.next(&seg);
-  if (!have) return;
+  if (warp == 0) ca_plan(s_off, p.batch, p.num_kv_heads * p.head_blocks, &s_plan, s_seg);
+  __syncthreads();
+  if (s_seg[0].b < 0) return;
 
   const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(ca_smem)) + warp * static_cast<uint32_t>(W::kRing);
   constexpr uint32_t kAcc = (kCaStages - 1) * kSlot;             // the warp's sums: in the last slot of its ring
   CaRows<POS> rows;
   const T* q0;
-  int first, heads, hq;
+  int first, heads, which = 0;
   uint32_t seen[kCaStages], far[kCaStages];                      // of the tiles in the ring, oldest first
   int64_t mine_last, next;                                       // where the rows of the last slot's tile lie, and the next one's
   int next_pos;
@@ -731,10 +756,10 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   // Starts on a segment: the tiles of all slots but the last one are on their way.
-  auto begin = [&]() {
+  auto begin = [&](const CaSegment& seg) {
     const int h = seg.unit / p.head_blocks, g0 = (seg.unit - h * p.head_blocks) * GT;
+    const int hq = h * p.group + g0;
     heads = min(GT, p.group - g0);
-    hq = h * p.group + g0;
     q0 = static_cast<const T*>(p.q) + seg.b * p.q_sb + hq * p.q_sh;
     rows.table = p.table + (static_cast<int64_t>(seg.b) * p.num_kv_heads + h) * p.max_pages;
     rows.rows = min(min(max(__ldg(p.lens + seg.b), 0), most), seg.tile1 * kCaTile);
@@ -755,20 +780,28 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
       if (s < kCaStages - 1) copy_in(s * kSlot, seen[s], mine[s]);
     }
     mine_last = mine[kCaStages - 1];
+    q_buffer ^= 1;
     if constexpr (sizeof(T) == 4) {
       float* q_shared = reinterpret_cast<float*>(ca_smem + WARPS * W::kRing) + q_buffer * (GT * (D + 4));
-      q_buffer ^= 1;
       for (int i = tid; i < GT * D; i += THREADS) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
-      if (POS && tid < GT) q_shared[GT * D + tid] = p.slopes && tid < heads ? __ldg(p.slopes + hq + tid) * 1.4426950408889634f : 0.f;
+      if (POS == 2 && tid < GT) q_shared[GT * D + tid] = tid < heads ? __ldg(p.slopes + hq + tid) * 1.4426950408889634f : 0.f;
       sums.start(p, q_shared, heads, hq);
     } else {
-      sums.start(p, q0, heads, hq);
+      uint8_t* q_shared = ca_smem + WARPS * W::kRing + q_buffer * (GT * Sums::kQ);
+      for (int i = tid; i < GT * D / 8; i += THREADS) {           // 16 bytes each
+        const int g = i / (D / 8), piece = i % (D / 8);
+        *reinterpret_cast<uint4*>(q_shared + g * Sums::kQ + piece * 16) =
+            g < heads ? *reinterpret_cast<const uint4*>(q0 + g * p.q_sh + piece * 8) : make_uint4(0, 0, 0, 0);
+      }
+      sums.start(p, static_cast<uint32_t>(__cvta_generic_to_shared(q_shared)), heads, hq);
     }
   };
-  begin();
+  begin(s_seg[0]);
+  __syncthreads();                         // the queries are there
   while (true) {
-    if constexpr (sizeof(T) == 4) __syncthreads();               // the queries are there
     copy_in(kAcc, seen[kCaStages - 1], mine_last);
+    const int next_seg = which == 2 ? 0 : which + 1;
+    if (tid == THREADS - 1) ca_next(s_off, &s_plan, &s_seg[3 - which - next_seg]);       // (while the rows come)
     int64_t second = place(first + (kCaStages + 1) * kCaTile);   // one tile further
 
     // ---- the warp's rows
@@ -796,12 +829,13 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
     sums.finish(p, rows, q0, heads, first, reinterpret_cast<float*>(ca_smem + warp * W::kRing + kAcc), s_m[warp], s_z[warp]);
 
     // ---- the next segment's rows start on their way, then the warps' sums meet
-    const CaSegment was = seg;
+    const CaSegment& was = s_seg[which];
     const int heads_was = heads;
-    const int64_t head0 = static_cast<int64_t>(was.b) * p.num_kv_heads * p.group + hq;
-    have = plan.next(&seg);
-    if (have) begin();
+    const bool have = s_seg[next_seg].b >= 0;
+    if (have) begin(s_seg[next_seg]);
     __syncthreads();
+    const int h_was = was.unit / p.head_blocks;
+    const int64_t head0 = (static_cast<int64_t>(was.b) * p.num_kv_heads + h_was) * p.group + (was.unit - h_was * p.head_blocks) * GT;
     // the output, or a partial result that the unit's last CTA joins with the others
     float* part = p.partials + static_cast<int64_t>(was.slot) * kCaPartial;
     for (int o = tid; o < heads_was * D; o += THREADS) {
@@ -827,10 +861,10 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
       }
     }
     if (!was.whole) {
-      __threadfence();
       __syncthreads();
       if (tid == 0) {
-        int32_t* counter = p.counters + static_cast<int64_t>(was.b) * plan.per_seq + was.unit;
+        __threadfence();                   // for the whole CTA, which the barrier has ordered before it
+        int32_t* counter = p.counters + static_cast<int64_t>(was.b) * s_plan.per_seq + was.unit;
         s_last = atomicAdd(counter, 1) == was.more;
         if (s_last) *counter = 0;          // everybody has arrived: ready for the next call
         __threadfence();
@@ -840,6 +874,7 @@ __global__ void __launch_bounds__(kCaThreads<T>) cache_attend_kernel(const __gri
     }
     if (!have) return;
     __syncthreads();                       // the sums have been read: the last slot may be filled
+    which = next_seg;
   }
 }
 
