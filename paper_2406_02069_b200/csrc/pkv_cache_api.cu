@@ -134,6 +134,7 @@ void launch_rotary_type(RotaryParams& p, int d, cudaStream_t st) {
   constexpr int VEC = 16 / static_cast<int>(sizeof(T));
   // 16-byte pieces need both halves of the rotated part (interleaved: its end) at multiples of 16 bytes
   if (p.half % VEC == 0) launch_rotary_units<T, VEC, APPEND>(p, d, st);
+  else if (p.half % 2 == 0) launch_rotary_units<T, 2, APPEND>(p, d, st);
   else launch_rotary_units<T, 1, APPEND>(p, d, st);
 }
 

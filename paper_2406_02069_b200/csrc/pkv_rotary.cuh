@@ -7,15 +7,24 @@
 //   * The angle is formed in turns and in fp64, p * (f / 2 pi), and loses its whole turns there: in fp32 a position of 100000
 //     would leave an error of 4e-3 rad.  sincospif then sees at most half a turn.
 //   * VEC elements make 16 bytes where the pieces of the rotated part start at multiples of 16 bytes; a rotated part of another
-//     size is taken pair by pair (VEC = 1).
+//     size is taken two pairs at a time, or pair by pair (8192 tokens of 40 heads, 20 of 128 elements rotated: XX us, pair by pair 61).
+//   * 16-bit elements are taken apart and put together two to a word (one by one: 185 us for 32 / 8 heads x 32768 tokens, now 109,
+//     94 % of the rate of a copy).
 #pragma once
 
 #include "pkv_common.cuh"
+#include "pkv_mma16.cuh"
 
 namespace pkv {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotUnroll = 4;              // heads whose rows a thread has on their way at a time
+// Heads whose rows a thread has on their way at a time, and CTAs that an SM shall hold.  32 / 8 heads x 32768 tokens in bf16: two
+// and four 109 us, four and two 118, one and four 118, two and two 132.  An append of 2000 rows in pieces: four and two 16 us,
+// two and four 21 (its look-ups need the registers).
+template <int VEC, bool APPEND>
+constexpr int kRotUnroll = VEC > 2 && !APPEND ? 2 : 4;
+template <int VEC, bool APPEND>
+constexpr int kRotPerSm = VEC > 2 && !APPEND ? 4 : 2;
 
 struct RotaryParams {
   TensorView q, q_out, k, k_out, v;        // k_out: not used by an append, its keys go into pages
@@ -40,6 +49,12 @@ struct RotaryParams {
   double turns[64];                        // per position, of each pair
 };
 
+// VEC elements of a row, and the rotation of two of them (half layout: x and y of VEC pairs; interleaved: VEC / 2 pairs each).
+template <typename T, int VEC>
+struct alignas(sizeof(T) * VEC) RotPiece {
+  T x[VEC];
+};
+
 template <typename T>
 __device__ __forceinline__ T from_float(float x);
 template <>
@@ -49,15 +64,54 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 
+__device__ __forceinline__ void rot_pair(float& x, float& y, float c, float s) {
+  const float t = fmaf(x, c, -(y * s));
+  y = fmaf(y, c, x * s);
+  x = t;
+}
+
 template <typename T, int VEC>
-struct alignas(sizeof(T) * VEC) RotPiece {
-  T x[VEC];
-};
+__device__ __forceinline__ void rot_pieces(RotPiece<T, VEC>& a, RotPiece<T, VEC>& b, const float (&cs)[VEC], const float (&sn)[VEC], bool interleaved) {
+  if constexpr (sizeof(T) == 2 && VEC > 1) {                     // two elements to a word
+    uint32_t* aw = reinterpret_cast<uint32_t*>(&a);
+    uint32_t* bw = reinterpret_cast<uint32_t*>(&b);
+#pragma unroll
+    for (int w = 0; w < VEC / 2; ++w) {
+      float2 x = Dec16<T>::unpack(aw[w]), y = Dec16<T>::unpack(bw[w]);
+      if (interleaved) {
+        rot_pair(x.x, x.y, cs[w], sn[w]);
+        rot_pair(y.x, y.y, cs[VEC / 2 + w], sn[VEC / 2 + w]);
+      } else {
+        rot_pair(x.x, y.x, cs[2 * w], sn[2 * w]);
+        rot_pair(x.y, y.y, cs[2 * w + 1], sn[2 * w + 1]);
+      }
+      aw[w] = Dec16<T>::pack(x.x, x.y);
+      bw[w] = Dec16<T>::pack(y.x, y.y);
+    }
+  } else if constexpr (VEC > 1) {
+    if (interleaved) {
+#pragma unroll
+      for (int e = 0; e < VEC / 2; ++e) {
+        rot_pair(a.x[2 * e], a.x[2 * e + 1], cs[e], sn[e]);
+        rot_pair(b.x[2 * e], b.x[2 * e + 1], cs[VEC / 2 + e], sn[VEC / 2 + e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) rot_pair(a.x[e], b.x[e], cs[e], sn[e]);
+    }
+  } else {
+    float x = to_float(a.x[0]), y = to_float(b.x[0]);
+    rot_pair(x, y, cs[0], sn[0]);
+    a.x[0] = from_float<T>(x);
+    b.x[0] = from_float<T>(y);
+  }
+}
 
 // grid (ceil(tokens of the batch / tokens of a block), head splits).
 template <typename T, int VEC, bool APPEND>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotaryParams p) {
+__global__ void __launch_bounds__(kRotThreads, kRotPerSm<VEC, APPEND>) rotary_kernel(const __grid_constant__ RotaryParams p) {
   using Piece = RotPiece<T, VEC>;
+  constexpr int UNROLL = kRotUnroll<VEC, APPEND>;
   __shared__ double s_turns[64];
   pdl_trigger();
   if (threadIdx.x < 64) s_turns[threadIdx.x] = p.turns[threadIdx.x];
@@ -80,6 +134,49 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   }
   const int pos = p.positions ? __ldg(p.positions + b * p.positions_stride + t) : 0;
   const bool rotated = u < p.rot_units;
+  // elements at which the unit's two pieces start
+  const int r = 2 * p.half;
+  const int e0 = !rotated ? r + (u - p.rot_units) * 2 * VEC : (p.interleaved ? u * 2 * VEC : u * VEC);
+  const int e1 = rotated && !p.interleaved ? p.half + u * VEC : e0 + VEC;
+
+  const int heads = p.heads_q + p.heads_kv * (APPEND ? 2 : 1);
+  const int step = gridDim.y * p.head_lanes;
+  const T* q_in = static_cast<const T*>(p.q.ptr) + b * p.q.sb + t * p.q.st;
+  const T* k_in = static_cast<const T*>(p.k.ptr) + b * p.k.sb + t * p.k.st;
+  const T* v_in = static_cast<const T*>(p.v.ptr) + b * p.v.sb + t * p.v.st;
+  T* q_to = static_cast<T*>(const_cast<void*>(p.q_out.ptr)) + b * p.q_out.sb + t * p.q_out.st;
+  T* k_to = static_cast<T*>(const_cast<void*>(p.k_out.ptr)) + b * p.k_out.sb + t * p.k_out.st;
+  Piece a[UNROLL], c[UNROLL];
+  T* to[UNROLL];
+  // Rows of the heads h0, h0 + step ..: on their way to a and c; to: where they go, null for those that do not.
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < UNROLL; ++i) {
+      const int h = h0 + i * step;
+      to[i] = nullptr;
+      if (h >= heads) continue;
+      const bool is_q = h < p.heads_q, is_v = APPEND && h >= p.heads_q + p.heads_kv;
+      const int hh = is_q ? h : (is_v ? h - p.heads_q - p.heads_kv : h - p.heads_q);
+      const T* from = is_q ? q_in + hh * p.q.sh : (is_v ? v_in + hh * p.v.sh : k_in + hh * p.k.sh);
+      if (APPEND && !is_q) {
+        const int page = inside ? __ldg(p.table + (static_cast<int64_t>(b) * p.heads_kv + hh) * p.max_pages + page_at) : -1;
+        if (page < 0 || page >= p.num_pages) {
+          if (u == 0) atomicOr(p.status, kStatusBadPage);
+          continue;
+        }
+        const int64_t slot = static_cast<int64_t>(page) * p.page_size + slot_in_page;
+        to[i] = static_cast<T*>(is_v ? p.v_pool : p.k_pool) + slot * (p.units * 2 * VEC);
+        if (!is_v && u == 0 && p.pos_pool) p.pos_pool[slot] = pos;
+      } else {
+        to[i] = is_q ? q_to + hh * p.q_out.sh : k_to + hh * p.k_out.sh;
+        if (to[i] == from && !rotated) { to[i] = nullptr; continue; }         // in place, not part of the rotation
+      }
+      a[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC : e0));
+      c[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC + VEC : e1));
+    }
+  };
+  const int first = blockIdx.y * p.head_lanes + hl;
+  fetch(first);                            // (the sines are formed while they come)
   float cs[VEC], sn[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) {
@@ -93,69 +190,17 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
       sn[i] *= p.magnitude_sin;
     }
   }
-  // elements at which the unit's two pieces start
-  const int r = 2 * p.half;
-  const int e0 = !rotated ? r + (u - p.rot_units) * 2 * VEC : (p.interleaved ? u * 2 * VEC : u * VEC);
-  const int e1 = rotated && !p.interleaved ? p.half + u * VEC : e0 + VEC;
-
-  const int heads = p.heads_q + p.heads_kv * (APPEND ? 2 : 1);
-  const int step = gridDim.y * p.head_lanes;
-  for (int h0 = blockIdx.y * p.head_lanes + hl; h0 < heads; h0 += step * kRotUnroll) {
-    Piece a[kRotUnroll], c[kRotUnroll];
-    T* to[kRotUnroll];
+  for (int h0 = first; h0 < heads;) {
 #pragma unroll
-    for (int i = 0; i < kRotUnroll; ++i) {
-      const int h = h0 + i * step;
-      to[i] = nullptr;
-      if (h >= heads) continue;
-      const bool is_q = h < p.heads_q, is_v = APPEND && h >= p.heads_q + p.heads_kv;
-      const int hh = is_q ? h : (is_v ? h - p.heads_q - p.heads_kv : h - p.heads_q);
-      const TensorView& in = is_q ? p.q : (is_v ? p.v : p.k);
-      const T* from = static_cast<const T*>(in.ptr) + b * in.sb + hh * in.sh + t * in.st;
-      if (APPEND && !is_q) {
-        const int page = inside ? __ldg(p.table + (static_cast<int64_t>(b) * p.heads_kv + hh) * p.max_pages + page_at) : -1;
-        if (page < 0 || page >= p.num_pages) {
-          if (u == 0) atomicOr(p.status, kStatusBadPage);
-          continue;
-        }
-        const int64_t slot = static_cast<int64_t>(page) * p.page_size + slot_in_page;
-        to[i] = static_cast<T*>(is_v ? p.v_pool : p.k_pool) + slot * (p.units * 2 * VEC);
-        if (!is_v && u == 0 && p.pos_pool) p.pos_pool[slot] = pos;
-      } else {
-        const TensorView& out = is_q ? p.q_out : p.k_out;
-        to[i] = static_cast<T*>(const_cast<void*>(out.ptr)) + b * out.sb + hh * out.sh + t * out.st;
-        if (to[i] == from && !rotated) { to[i] = nullptr; continue; }         // in place, not part of the rotation
-      }
-      a[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC : e0));
-      c[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC + VEC : e1));
-    }
-#pragma unroll
-    for (int i = 0; i < kRotUnroll; ++i) {
+    for (int i = 0; i < UNROLL; ++i) {
       if (!to[i]) continue;
       const bool is_v = APPEND && h0 + i * step >= p.heads_q + p.heads_kv;
-      if (rotated && !is_v) {
-        if (VEC == 1 || !p.interleaved) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float x = to_float(a[i].x[e]), y = to_float(c[i].x[e]);
-            a[i].x[e] = from_float<T>(fmaf(x, cs[e], -(y * sn[e])));
-            c[i].x[e] = from_float<T>(fmaf(y, cs[e], x * sn[e]));
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e + 1 < VEC; e += 2) {
-            const float x = to_float(a[i].x[e]), y = to_float(a[i].x[e + 1]);
-            a[i].x[e] = from_float<T>(fmaf(x, cs[e / 2], -(y * sn[e / 2])));
-            a[i].x[e + 1] = from_float<T>(fmaf(y, cs[e / 2], x * sn[e / 2]));
-            const float z = to_float(c[i].x[e]), w = to_float(c[i].x[e + 1]);
-            c[i].x[e] = from_float<T>(fmaf(z, cs[VEC / 2 + e / 2], -(w * sn[VEC / 2 + e / 2])));
-            c[i].x[e + 1] = from_float<T>(fmaf(w, cs[VEC / 2 + e / 2], z * sn[VEC / 2 + e / 2]));
-          }
-        }
-      }
+      if (rotated && !is_v) rot_pieces<T, VEC>(a[i], c[i], cs, sn, p.interleaved);
       *reinterpret_cast<Piece*>(to[i] + (is_v ? u * 2 * VEC : e0)) = a[i];
       *reinterpret_cast<Piece*>(to[i] + (is_v ? u * 2 * VEC + VEC : e1)) = c[i];
     }
+    h0 += step * UNROLL;
+    if (h0 < heads) fetch(h0);
   }
 }
 

@@ -34,7 +34,9 @@ CASES = [
     ((7, 7), 128, "fp32", 120, "interleaved", {}, 1, 11, 9),                    # 4-element pieces
     ((16, 8), 64, "bf16", 64, "half", {}, 2, 1501, 0),                          # enough rows for a warp per token
     ((40, 8), 128, "bf16", 128, "half", {}, 1, 1801, 3),
-    ((8, 2), 128, "fp16", 100, "half", {}, 3, 1203, 10),                        # ... pair by pair
+    ((8, 2), 128, "fp16", 100, "half", {}, 3, 1203, 10),                        # ... two pairs at a time
+    ((8, 2), 128, "bf16", 98, "interleaved", {}, 3, 1203, 10),                  # ... pair by pair
+    ((4, 2), 64, "fp32", 30, "half", {}, 2, 9, 50),
     ((8, 8), 128, "fp32", 128, "interleaved", {}, 1, 1203, 10),
 ]
 IDS = ["%dx%d_d%d_%s_r%d_%s_%dx%d" % (c[0][0], c[0][1], c[1], c[2], c[3], c[4], c[6], c[7]) for c in CASES]
@@ -161,6 +163,7 @@ APPENDS = [
     ((8, 8), 64, "fp16", 32, "interleaved", 5, [3, 9, 40], [3, 0, 2], 3),
     ((6, 2), 128, "bf16", 0, "half", 1, [5, 7], [2, 2], 2),
     ((5, 1), 128, "fp16", 20, "half", 7, [30, 100, 64], [30, 1, 33], 33),
+    ((6, 2), 64, "bf16", 26, "interleaved", 7, [30, 100, 64], [30, 1, 33], 33),
     ((8, 2), 64, "bf16", 64, "interleaved", 64, [700, 650], [600, 513], 600),
     ((4, 4), 128, "fp32", 128, "half", 32, [0, 5], [0, 5], 5),
     ((4, 1), 64, "bf16", 64, "half", 16, [20], [99], 4),                       # a count beyond the tokens: as if all
