@@ -269,7 +269,7 @@ int run_fork(const pkv_config* c, const pkv_cache* from, const pkv_cache* to, Pa
     launch_pdl(pages_carry_kernel, dim3(p.to_batch + (p.parents ? p.from_batch : 0), p.layers), dim3(kPgCarryThreads), 0, st, p);
   if (const int rc = launch_cluster(pages_deal_kernel, p, st)) return rc;
   if (p.parents) {
-    launch_pdl(pages_copy_kernel, dim3(p.to_batch, p.layers, p.num_kv_heads), dim3(kPgCopyThreads), 0, st, p);
+    launch_pdl(pages_copy_kernel, dim3(p.to_batch, p.layers), dim3(kPgCarryThreads), 0, st, p);
     note_output(from->k_pool, pool_bytes(c, from));
     note_output(from->v_pool, pool_bytes(c, from));
   }

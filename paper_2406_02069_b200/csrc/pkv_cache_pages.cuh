@@ -5,9 +5,10 @@
 //   1. pages_carry_kernel   (`to` is another set of arrays, or sequences change places) tables, lens and refs of `to` from those
 //      of `from`, counts of shared pages adjusted.  Grid over the table, bound by its bytes.
 //   2. pages_deal_kernel / pages_pair_kernel   one cluster of 8 CTAs, because every page's place depends on all pages below it:
-//      each CTA sums its eighth of the requests and of refs, the eighths meet through distributed shared memory, and the free
-//      pages' ranks are found in a second pass over the eighths that are needed.  Bound by the latency of those passes; refs
-//      come from the L2 in 16-byte loads.
+//      each warp counts its consecutive share of refs, the sums meet in the CTA and, through distributed shared memory, in the
+//      cluster, and a second look at the share gives each free page its rank.  Bound by the latency of those steps; refs come from
+//      the L2 in 16-byte loads.  (A scan of the CTA for every 4096 pages, or shares of threads, whose entries of the lists lie in
+//      sectors of their own: 45 us for 290000 pages, XX this way.)
 //   3. pages_copy_kernel / pages_move_kernel   rows of part-filled pages to their copies, or whole pages downwards together with the
 //      tables that name them.  Bound by memory.
 // All or nothing: step 2 knows whether there is room before it changes anything; where step 1 has already written in place
@@ -226,39 +227,43 @@ __device__ __forceinline__ uint32_t pg_free4(const int32_t* refs, bool aligned, 
   return bits;
 }
 
-// This CTA's eighth of 0 .. n - 1, its borders multiples of four.
-__device__ __forceinline__ void pg_share(int64_t n, int rank, int64_t* lo, int64_t* hi) {
-  const int64_t per = ((n + kPgCluster - 1) / kPgCluster + 3) / 4 * 4;
-  *lo = min(n, per * rank);
-  *hi = min(n, per * (rank + 1));
+// A warp's share of the pool: tiles of 128 pages, four to a lane.
+constexpr int kPgTile = 128;
+constexpr int kPgWarps = kPgCluster * kPgThreads / 32;
+__device__ __forceinline__ void pg_share(int64_t pages, int rank, int64_t* lo, int64_t* hi) {
+  const int64_t per = ((pages + kPgWarps - 1) / kPgWarps + kPgTile - 1) / kPgTile * kPgTile;
+  const int64_t worker = rank * (kPgThreads / 32) + (threadIdx.x >> 5);
+  *lo = min(pages, per * worker);
+  *hi = min(pages, per * (worker + 1));
 }
 
-// Free pages among lo .. hi - 1, counted by the CTA.
-__device__ __forceinline__ int pg_count_free(PgShared& s, const int32_t* refs, int64_t lo, int64_t hi) {
-  const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
-  int free = 0, total;
-  for (int64_t i = lo + threadIdx.x * 4; i < hi; i += kPgThreads * 4) free += __popc(pg_free4(refs, aligned, i, hi));
-  pg_scan(s, free, &total);
-  return total;
+// Free pages among lo .. hi - 1, lo the start of a tile; the same in all lanes.
+__device__ __forceinline__ int pg_count_free(const int32_t* refs, bool aligned, int64_t lo, int64_t hi) {
+  int free = 0;
+#pragma unroll 4
+  for (int64_t base = lo; base < hi; base += kPgTile) free += __popc(pg_free4(refs, aligned, base + (threadIdx.x & 31) * 4, hi));
+  return __reduce_add_sync(0xffffffffu, free);
 }
 
-// Calls take(page, rank) for the free pages among lo .. hi - 1 whose rank (from `ahead` on) is below `need`.
-template <typename F>
-__device__ __forceinline__ void pg_rank_free(PgShared& s, const int32_t* refs, int64_t lo, int64_t hi, int ahead, int need, F&& take) {
-  const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
-  for (int64_t base = lo; base < hi && ahead < need; base += kPgThreads * 4) {     // (uniform over the CTA)
-    const int64_t i = base + threadIdx.x * 4;
-    const uint32_t bits = i < hi ? pg_free4(refs, aligned, i, hi) : 0u;
-    int total;
-    int rank = ahead + pg_scan(s, __popc(bits), &total);
+// What the warps ahead have of a number that each warp has; *total: all of them.
+__device__ __forceinline__ int pg_ahead(PgShared& s, int mine, int* total) {
+  int cta, ahead;
+  const int run = pg_scan(s, (threadIdx.x & 31) == 0 ? mine : 0, &cta);
+  pg_cluster(s, cta, &ahead, total);
+  return ahead + __shfl_sync(0xffffffffu, run, 0);
+}
+
+// What the lanes ahead have; *total: all of them.
+__device__ __forceinline__ int pg_lanes_ahead(int mine, int* total) {
+  const int lane = threadIdx.x & 31;
+  int run = mine;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if ((bits >> e) & 1u) {
-        if (rank < need) take(static_cast<int32_t>(i + e), rank);
-        ++rank;
-      }
-    ahead += total;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += y;
   }
+  *total = __shfl_sync(0xffffffffu, run, 31);
+  return run - mine;
 }
 
 // One cluster.  Requests are counted, free pages found and dealt out; lens, granted and the new table entries of `to` are written.
@@ -286,15 +291,15 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
     if (s_parent[c] >= 0 && s_child[s_parent[c]] != c) s_parent[c] |= 1 << 30;
   __syncthreads();
   const int64_t units = static_cast<int64_t>(p.layers) * p.to_batch;
-  int64_t lo, hi;
-  pg_share(units, rank, &lo, &hi);
+  const int worker = rank * kPgThreads + tid;
+  constexpr int kWorkers = kPgCluster * kPgThreads;
   auto child = [&](int64_t unit) {
     const int l = static_cast<int>(unit / p.to_batch), c = static_cast<int>(unit - static_cast<int64_t>(l) * p.to_batch);
     const int x = s_parent[c];
     return pg_child(p, l, c, x < 0 ? -1 : x & ~(1 << 30), x >= 0 && !(x >> 30));
   };
   // requests of every unit; each thread has consecutive ones
-  const int64_t per = (hi - lo + kPgThreads - 1) / kPgThreads, u0 = min(hi, lo + per * tid), u1 = min(hi, u0 + per);
+  const int64_t per = (units + kWorkers - 1) / kWorkers, u0 = min(units, per * worker), u1 = min(units, u0 + per);
   int64_t mine = 0;
   for (int64_t u = u0; u < u1; ++u) {
     const PgChild x = child(u);
@@ -317,11 +322,12 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   int flags = 0;
 #pragma unroll
   for (int c = 0; c < kPgCluster; ++c) flags |= *cluster.map_shared_rank(&s.flag, c);
+  const bool aligned = reinterpret_cast<uintptr_t>(p.to.refs) % 16 == 0;
   int64_t flo, fhi;
   pg_share(p.num_pages, rank, &flo, &fhi);
-  const int free_here = pg_count_free(s, p.to.refs, flo, fhi);
-  int free_ahead, free_all;
-  pg_cluster(s, free_here, &free_ahead, &free_all);
+  const int my_free = pg_count_free(p.to.refs, aligned, flo, fhi);
+  int free_all;
+  int place = pg_ahead(s, my_free, &free_all);                   // the rank of this warp's first free page
   const bool met = flags == 0 && static_cast<uint32_t>(need) <= static_cast<uint32_t>(free_all);
   if (rank == 0 && tid == 0) {
     p.state[0] = met ? 1 : 0;
@@ -332,10 +338,22 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
       for (int64_t u = u0; u < u1; ++u) p.granted[u] = 0;
     return;
   }
-  pg_rank_free(s, p.to.refs, flo, fhi, free_ahead, need, [&](int32_t page, int r) {
-    p.list[r] = page;
-    p.to.refs[page] = 1;
-  });
+  for (int64_t base = flo; base < fhi && my_free && place < need; base += kPgTile) {       // (uniform over the warp)
+    const int64_t i = base + (tid & 31) * 4;
+    const uint32_t bits = pg_free4(p.to.refs, aligned, i, fhi);
+    int total;
+    int r = place + pg_lanes_ahead(__popc(bits), &total);
+    place += total;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if ((bits >> e) & 1u) {
+        if (r < need) {
+          p.list[r] = static_cast<int32_t>(i + e);
+          p.to.refs[i + e] = 1;
+        }
+        ++r;
+      }
+  }
   int64_t off = ahead + static_cast<int64_t>(run_low) + (static_cast<int64_t>(run_high) << 16);
   for (int64_t u = u0; u < u1; ++u) {
     const PgChild x = child(u);
@@ -343,18 +361,31 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
     off += static_cast<int64_t>(x.pages - x.keeps) * p.num_kv_heads;
   }
   cluster.sync();                          // list and offsets are there (and so are everybody's reads of lens)
-  // table entries: a warp per head of a unit
+  // table entries: a lane has a head of a unit; where that needs many pages, its warp writes them together
+  // (a warp per head throughout: 79 us for 64 sequences x 32 layers x 8 heads, XX this way)
+  constexpr int kAlone = 4;
   const int lane = tid & 31;
   const int64_t heads = units * p.num_kv_heads;
-  for (int64_t i = static_cast<int64_t>(rank) * (kPgThreads / 32) + (tid >> 5); i < heads; i += kPgCluster * (kPgThreads / 32)) {
-    const int64_t u = i / p.num_kv_heads;
-    const int h = static_cast<int>(i - u * p.num_kv_heads);
-    const PgChild x = child(u);
-    const int fresh = x.pages - x.keeps;
-    if (!fresh) continue;
-    const int32_t* pages = p.list + __ldcg(p.unit_off + u) + static_cast<int64_t>(h) * fresh;
-    int32_t* table = p.to.tables + (u * p.num_kv_heads + h) * p.max_pages + x.keeps;
-    for (int j = lane; j < fresh; j += 32) table[j] = __ldcg(pages + j);
+  for (int64_t i0 = worker - lane; i0 < heads; i0 += kWorkers) {
+    const int64_t i = i0 + lane;
+    const int32_t* pages = p.list;
+    int32_t* table = p.to.tables;
+    int fresh = 0;
+    if (i < heads) {
+      const int64_t u = i / p.num_kv_heads;
+      const PgChild x = child(u);
+      fresh = x.pages - x.keeps;
+      if (fresh) pages += __ldcg(p.unit_off + u) + (i - u * p.num_kv_heads) * fresh;
+      table += i * p.max_pages + x.keeps;
+    }
+    if (fresh <= kAlone)
+      for (int j = 0; j < fresh; ++j) table[j] = __ldcg(pages + j);
+    for (unsigned many = __ballot_sync(0xffffffffu, fresh > kAlone); many; many &= many - 1) {
+      const int l = __ffs(many) - 1, n = __shfl_sync(0xffffffffu, fresh, l);
+      const int32_t* from = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(pages), l));
+      int32_t* to = reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(table), l));
+      for (int j = lane; j < n; j += 32) to[j] = __ldcg(from + j);
+    }
   }
   cluster.sync();                          // lens of `from` may be those of `to`: they change behind everybody's last look
   for (int64_t u = u0; u < u1; ++u) {
@@ -365,16 +396,16 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------ 3. rows of a part-filled page to its copies
-// grid (sequences of `to`, layers, heads).  If the call was not met: puts `to` back (in place), a share per CTA.
-__global__ void __launch_bounds__(kPgCopyThreads) pages_copy_kernel(const __grid_constant__ PagesParams p) {
+// grid (sequences of `to`, layers).  If the call was not met: puts `to` back (in place), a share per CTA.
+__global__ void __launch_bounds__(kPgCarryThreads) pages_copy_kernel(const __grid_constant__ PagesParams p) {
   __shared__ int s_first;
   pdl_trigger();
   pdl_wait();
-  const int c = blockIdx.x, l = blockIdx.y, h = blockIdx.z;
+  const int c = blockIdx.x, l = blockIdx.y;
   if (!p.state[0]) {
     if (!p.in_place) return;
-    const int64_t cta = (static_cast<int64_t>(h) * gridDim.y + l) * gridDim.x + c, ctas = static_cast<int64_t>(gridDim.x) * gridDim.y * gridDim.z;
-    const int64_t at = cta * kPgCopyThreads + threadIdx.x, step = ctas * kPgCopyThreads;
+    const int64_t at = (static_cast<int64_t>(l) * gridDim.x + c) * kPgCarryThreads + threadIdx.x;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * gridDim.y * kPgCarryThreads;
     const int64_t entries = static_cast<int64_t>(p.layers) * p.from_batch * p.num_kv_heads * p.max_pages;
     for (int64_t i = at; i < entries; i += step) p.home.tables[i] = p.from.tables[i];
     for (int64_t i = at; i < p.num_pages; i += step) p.home.refs[i] = p.from.refs[i];
@@ -384,31 +415,33 @@ __global__ void __launch_bounds__(kPgCopyThreads) pages_copy_kernel(const __grid
   if (parent < 0) return;
   if (threadIdx.x == 0) s_first = 1;
   __syncthreads();
-  for (int i = threadIdx.x; i < c; i += kPgCopyThreads)
+  for (int i = threadIdx.x; i < c; i += kPgCarryThreads)
     if (__ldg(p.parents + i) == parent) s_first = 0;
   __syncthreads();
   const PgChild x = pg_child(p, l, c, parent, s_first != 0);
   if (x.first || !x.part) return;
-  const int src = p.from.tables[((static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads + h) * p.max_pages + x.full];
-  const int dst = p.to.tables[((static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads + h) * p.max_pages + x.full];
-  if (src < 0 || src >= p.num_pages) {
-    if (threadIdx.x == 0) atomicOr(p.status, kStatusBadPage);
-    return;
-  }
+  const int32_t* src_table = p.from.tables + (static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads * p.max_pages + x.full;
+  const int32_t* dst_table = p.to.tables + (static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads * p.max_pages + x.full;
   const int64_t page = static_cast<int64_t>(p.page_size) * p.row_pieces;
-  const uint4* ks = static_cast<const uint4*>(p.k_pool) + src * page;
-  const uint4* vs = static_cast<const uint4*>(p.v_pool) + src * page;
-  uint4* kd = static_cast<uint4*>(p.k_pool) + dst * page;
-  uint4* vd = static_cast<uint4*>(p.v_pool) + dst * page;
-  const int64_t pieces = static_cast<int64_t>(x.part) * p.row_pieces;
-  for (int64_t i = threadIdx.x; i < pieces; i += kPgCopyThreads) {
-    const uint4 a = ks[i], b = vs[i];
-    kd[i] = a;
-    vd[i] = b;
+  const int pieces = x.part * p.row_pieces;
+  for (int64_t i = threadIdx.x; i < static_cast<int64_t>(pieces) * p.num_kv_heads; i += kPgCarryThreads) {
+    const int64_t h = i / pieces, piece = i - h * pieces;
+    const int src = src_table[h * p.max_pages], dst = dst_table[h * p.max_pages];
+    if (src < 0 || src >= p.num_pages) {
+      if (piece == 0) atomicOr(p.status, kStatusBadPage);
+      continue;
+    }
+    const int64_t a = src * page + piece, b = dst * page + piece;
+    static_cast<uint4*>(p.k_pool)[b] = static_cast<const uint4*>(p.k_pool)[a];
+    static_cast<uint4*>(p.v_pool)[b] = static_cast<const uint4*>(p.v_pool)[a];
   }
   if (p.pos_pool)
-    for (int i = threadIdx.x; i < x.part; i += kPgCopyThreads)
-      p.pos_pool[static_cast<int64_t>(dst) * p.page_size + i] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + i];
+    for (int64_t i = threadIdx.x; i < static_cast<int64_t>(x.part) * p.num_kv_heads; i += kPgCarryThreads) {
+      const int64_t h = i / x.part, row = i - h * x.part;
+      const int src = src_table[h * p.max_pages], dst = dst_table[h * p.max_pages];
+      if (src < 0 || src >= p.num_pages) continue;
+      p.pos_pool[static_cast<int64_t>(dst) * p.page_size + row] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + row];
+    }
 }
 
 // ------------------------------------------------------------------ compaction
@@ -421,44 +454,42 @@ __global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_con
   pdl_trigger();
   const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
   pdl_wait();
-  int64_t lo, hi;
+  const int32_t* refs = p.from.refs;
+  const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
+  int64_t lo, hi;                          // this warp's pages
   pg_share(p.num_pages, rank, &lo, &hi);
-  const int free_here = pg_count_free(s, p.from.refs, lo, hi);
-  int free_ahead, free_all;
-  pg_cluster(s, free_here, &free_ahead, &free_all);
-  const int used = p.num_pages - free_all;
-  // free pages below `used`, in this CTA's share and the ones ahead of it
+  const int free = pg_count_free(refs, aligned, lo, hi);
+  int all, moves;
+  pg_ahead(s, free, &all);
+  const int used = p.num_pages - all;
+  // free pages below `used` and used ones from there on, ahead of this warp's; as many in all
   const int64_t cut = min(max(static_cast<int64_t>(used), lo), hi);
-  const int holes_here = pg_count_free(s, p.from.refs, lo, cut);
-  int holes_ahead, moves;
-  pg_cluster(s, holes_here, &holes_ahead, &moves);
+  const int holes = cut == hi ? free : (cut == lo ? 0 : pg_count_free(refs, aligned, lo, cut));
+  int mover = pg_ahead(s, static_cast<int>(hi - cut) - (free - holes), &moves), hole = pg_ahead(s, holes, &moves);
   if (rank == 0 && tid == 0) {
     p.state[0] = used;
     p.state[1] = moves;
     if (p.used) *p.used = used;
   }
-  pg_rank_free(s, p.from.refs, lo, cut, holes_ahead, moves, [&](int32_t page, int r) { p.list[r] = page; });
-  // used pages from `used` on: their rank is their distance from `used` less the free ones between
-  const int movers_here = static_cast<int>(hi - cut) - (free_here - holes_here);
-  int movers_ahead, movers;
-  pg_cluster(s, movers_here, &movers_ahead, &movers);
-  const bool aligned = reinterpret_cast<uintptr_t>(p.from.refs) % 16 == 0;
-  int ahead = movers_ahead;
-  for (int64_t base = cut / 4 * 4; base < hi; base += kPgThreads * 4) {            // (uniform over the CTA)
-    const int64_t i = base + tid * 4;
-    uint32_t there = 0, bits = 0;
-    if (i < hi) {
-      there = (i + 4 <= hi ? 15u : (1u << (hi - i)) - 1u) & ~(i < cut ? (1u << (cut - i)) - 1u : 0u);
-      bits = there & ~pg_free4(p.from.refs, aligned, i, hi);
-    }
+  for (int64_t base = lo; base < hi; base += kPgTile) {
+    const int64_t i = base + (tid & 31) * 4;
+    const uint32_t free4 = pg_free4(refs, aligned, i, hi);
+    const uint32_t there = i >= hi ? 0u : (i + 4 <= hi ? 15u : (1u << (hi - i)) - 1u);
+    const uint32_t below = i >= cut ? 0u : (i + 4 <= cut ? 15u : (1u << (cut - i)) - 1u);
+    const uint32_t hole4 = free4 & below, mover4 = there & ~below & ~free4;
     int total;
-    int r = ahead + pg_scan(s, __popc(bits), &total);
+    int h = pg_lanes_ahead(__popc(hole4) | __popc(mover4) << 16, &total);
+    int m = mover + (h >> 16);
+    h = hole + (h & 0xffff);
+    hole += total & 0xffff;
+    mover += total >> 16;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if ((bits >> e) & 1u) p.second[r++] = static_cast<int32_t>(i + e);
-      else if ((there >> e) & 1u) p.place[i + e] = static_cast<int32_t>(i + e);    // free: nothing should name it
+      const int32_t page = static_cast<int32_t>(i + e);
+      if ((hole4 >> e) & 1u) p.list[h++] = page;
+      if ((mover4 >> e) & 1u) p.second[m++] = page;
+      if ((free4 & ~below) >> e & 1u) p.place[page] = page;       // nothing should name it
     }
-    ahead += total;
   }
   cluster.sync();                          // both lists are there
   for (int m = rank * kPgThreads + tid; m < moves; m += kPgCluster * kPgThreads) p.place[__ldcg(p.second + m)] = __ldcg(p.list + m);
@@ -476,10 +507,20 @@ __global__ void __launch_bounds__(kPgCopyThreads) pages_move_kernel(const __grid
     const uint4* vs = static_cast<const uint4*>(p.v_pool) + src * page;
     uint4* kd = static_cast<uint4*>(p.k_pool) + dst * page;
     uint4* vd = static_cast<uint4*>(p.v_pool) + dst * page;
-    for (int64_t i = threadIdx.x; i < page; i += kPgCopyThreads) {
+    for (int64_t i = threadIdx.x; i < page; i += 2 * kPgCopyThreads) {
+      const bool two = i + kPgCopyThreads < page;
       const uint4 a = ks[i], b = vs[i];
+      uint4 c = make_uint4(0, 0, 0, 0), d = c;
+      if (two) {
+        c = ks[i + kPgCopyThreads];
+        d = vs[i + kPgCopyThreads];
+      }
       kd[i] = a;
       vd[i] = b;
+      if (two) {
+        kd[i + kPgCopyThreads] = c;
+        vd[i + kPgCopyThreads] = d;
+      }
     }
     if (p.pos_pool)
       for (int i = threadIdx.x; i < p.page_size; i += kPgCopyThreads)
