@@ -115,11 +115,11 @@ void launch_rotary_units(RotaryParams& p, int d, cudaStream_t st) {
   const int64_t tokens = static_cast<int64_t>(p.batch) * p.tokens;
   const int room = kRotThreads / p.units;
   int splits = 1;
-  // Enough rows to fill the device: a warp's lanes stay with a token and go through its heads, so that its sines are formed
-  // once per 32 / units heads.  Fewer: a lane per row, so that nothing is done in turn.
+  // Enough rows to fill the device: at most a warp's lanes, four to a head's unit, stay with a token and go through its heads, so
+  // that its sines are formed four times over.  Fewer: lanes for every row, so that nothing is done in turn.
   const int sms = std::max(1, device_sm_count());
   if (tokens * heads * p.units > static_cast<int64_t>(sms) * 4096) {
-    p.head_lanes = std::max(1, 32 / p.units);
+    p.head_lanes = std::max(1, std::min(4, 32 / p.units));
   } else {
     p.head_lanes = 1;
     while (p.head_lanes < heads && p.head_lanes < room) p.head_lanes *= 2;

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_refs_kernel(const __gri
 // grid (sequences of `to` and, where there are parents, of `from`; layers).  Entries that children keep are written to `to`;
 // a page gains a count for every child behind its first and loses one for a sequence without children.
 __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __grid_constant__ PagesParams p) {
-  __shared__ int s_parent, s_first;
+  __shared__ int s_first;
   pdl_trigger();
   pdl_wait();
   const int l = blockIdx.y, c = blockIdx.x;
@@ -125,17 +125,17 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
     for (int64_t i = at; i < p.num_pages; i += static_cast<int64_t>(gridDim.x) * gridDim.y * kPgCarryThreads) p.to.refs[i] = p.from.refs[i];
   }
   if (c < p.to_batch) {
-    if (threadIdx.x == 0) {
-      s_parent = pg_parent(p, c);
-      s_first = 1;
-    }
-    __syncthreads();
-    const int parent = s_parent;
-    if (p.parents)
+    const int parent = pg_parent(p, c);
+    bool first = true;
+    if (p.parents) {
+      if (threadIdx.x == 0) s_first = 1;
+      __syncthreads();
       for (int i = threadIdx.x; i < c; i += kPgCarryThreads)
         if (__ldg(p.parents + i) == parent) s_first = 0;
-    __syncthreads();
-    const PgChild x = pg_child(p, l, c, parent, s_first != 0);
+      __syncthreads();
+      first = s_first != 0;
+    }
+    const PgChild x = pg_child(p, l, c, parent, first);
     if (parent < 0) return;
     const int64_t src = (static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads * p.max_pages;
     const int64_t dst = (static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads * p.max_pages;
@@ -168,49 +168,47 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
 
 // ------------------------------------------------------------------ 2. sums and ranks over a cluster
 struct PgShared {
-  int32_t warp[32];
-  int32_t block;                           // this CTA's sum, read by the others
+  long long warp[32];
+  int32_t block[2];                        // this CTA's sums, read by the others; each is used once
   int32_t flag;
 };
 
 // Exclusive running sum over the CTA's threads; *total: the CTA's sum.  Everybody takes part.
-__device__ __forceinline__ int pg_scan(PgShared& s, int x, int* total) {
+template <typename I>
+__device__ __forceinline__ I pg_scan(PgShared& s, I x, I* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int run = x;
+  I run = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, run, o);
+    const I y = __shfl_up_sync(0xffffffffu, run, o);
     if (lane >= o) run += y;
   }
   __syncthreads();                         // the last call's sums have been read
   if (lane == 31) s.warp[warp] = run;
   __syncthreads();
-  int w = s.warp[lane];
+  I w = static_cast<I>(s.warp[lane]);
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, w, o);
+    const I y = __shfl_up_sync(0xffffffffu, w, o);
     if (lane >= o) w += y;
   }
   *total = __shfl_sync(0xffffffffu, w, 31);
-  const int ahead = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
-  return run - x + (warp ? ahead : 0);
+  const I ahead = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+  return run - x + (warp ? ahead : I(0));
 }
 
-// Sums of the CTAs of a cluster: what the CTAs ahead have, and all of them.
-__device__ __forceinline__ void pg_cluster(PgShared& s, int mine, int* ahead, int* total) {
+// What the CTAs ahead have of one of the sums, and all of them; behind a barrier of the cluster.
+__device__ __forceinline__ void pg_cluster(PgShared& s, int which, int* ahead, int* total) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
-  if (threadIdx.x == 0) s.block = mine;
-  cluster.sync();
   *ahead = *total = 0;
   const int rank = static_cast<int>(cluster.block_rank());
 #pragma unroll
   for (int c = 0; c < kPgCluster; ++c) {
-    const int x = *cluster.map_shared_rank(&s.block, c);
+    const int x = *cluster.map_shared_rank(&s.block[which], c);
     if (c < rank) *ahead += x;
     *total += x;
   }
-  cluster.sync();                          // everybody has read
 }
 
 // Four consecutive refs from `i` on (a multiple of four) as bits of free pages; pages behind `end` are not free.
@@ -237,21 +235,23 @@ __device__ __forceinline__ void pg_share(int64_t pages, int rank, int64_t* lo, i
   *hi = min(pages, per * (worker + 1));
 }
 
-// Free pages among lo .. hi - 1, lo the start of a tile; the same in all lanes.
-__device__ __forceinline__ int pg_count_free(const int32_t* refs, bool aligned, int64_t lo, int64_t hi) {
-  int free = 0;
+// Free pages of a warp's share.  The bits of its first eight tiles stay with the lane, so that a second look needs no loads there.
+struct PgFree {
+  uint32_t bits = 0;
+  __device__ __forceinline__ int count(const int32_t* refs, bool aligned, int64_t lo, int64_t hi) {
+    int free = 0;
+    const int64_t mine = lo + (threadIdx.x & 31) * 4;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) bits |= pg_free4(refs, aligned, mine + t * kPgTile, hi) << (4 * t);
+    free = __popc(bits);
 #pragma unroll 4
-  for (int64_t base = lo; base < hi; base += kPgTile) free += __popc(pg_free4(refs, aligned, base + (threadIdx.x & 31) * 4, hi));
-  return __reduce_add_sync(0xffffffffu, free);
-}
-
-// What the warps ahead have of a number that each warp has; *total: all of them.
-__device__ __forceinline__ int pg_ahead(PgShared& s, int mine, int* total) {
-  int cta, ahead;
-  const int run = pg_scan(s, (threadIdx.x & 31) == 0 ? mine : 0, &cta);
-  pg_cluster(s, cta, &ahead, total);
-  return ahead + __shfl_sync(0xffffffffu, run, 0);
-}
+    for (int64_t i = mine + 8 * kPgTile; i < hi; i += kPgTile) free += __popc(pg_free4(refs, aligned, i, hi));
+    return __reduce_add_sync(0xffffffffu, free);
+  }
+  __device__ __forceinline__ uint32_t tile(const int32_t* refs, bool aligned, int64_t i, int64_t hi, int t) const {
+    return t < 8 ? (bits >> (4 * t)) & 15u : pg_free4(refs, aligned, i, hi);
+  }
+};
 
 // What the lanes ahead have; *total: all of them.
 __device__ __forceinline__ int pg_lanes_ahead(int mine, int* total) {
@@ -277,25 +277,27 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
   pdl_wait();
   if (tid == 0) s.flag = 0;
-  for (int b = tid; b < p.from_batch; b += kPgThreads) s_child[b] = INT32_MAX;
-  __syncthreads();
   int bad = 0;                             // bit 0: a parent outside the batch, bit 1: a sequence too long for its table
-  for (int c = tid; c < p.to_batch; c += kPgThreads) {
-    const int parent = pg_parent(p, c);
-    if (p.parents && parent < 0 && __ldg(p.parents + c) != -1) bad |= 1;
-    if (parent >= 0) atomicMin(&s_child[parent], c);
-    s_parent[c] = parent;
+  if (p.parents) {
+    for (int b = tid; b < p.from_batch; b += kPgThreads) s_child[b] = INT32_MAX;
+    __syncthreads();
+    for (int c = tid; c < p.to_batch; c += kPgThreads) {
+      const int parent = pg_parent(p, c);
+      if (parent < 0 && __ldg(p.parents + c) != -1) bad |= 1;
+      if (parent >= 0) atomicMin(&s_child[parent], c);
+      s_parent[c] = parent;
+    }
+    __syncthreads();
+    for (int c = tid; c < p.to_batch; c += kPgThreads)
+      if (s_parent[c] >= 0 && s_child[s_parent[c]] != c) s_parent[c] |= 1 << 30;
   }
-  __syncthreads();
-  for (int c = tid; c < p.to_batch; c += kPgThreads)
-    if (s_parent[c] >= 0 && s_child[s_parent[c]] != c) s_parent[c] |= 1 << 30;
   __syncthreads();
   const int64_t units = static_cast<int64_t>(p.layers) * p.to_batch;
   const int worker = rank * kPgThreads + tid;
   constexpr int kWorkers = kPgCluster * kPgThreads;
   auto child = [&](int64_t unit) {
     const int l = static_cast<int>(unit / p.to_batch), c = static_cast<int>(unit - static_cast<int64_t>(l) * p.to_batch);
-    const int x = s_parent[c];
+    const int x = p.parents ? s_parent[c] : c;
     return pg_child(p, l, c, x < 0 ? -1 : x & ~(1 << 30), x >= 0 && !(x >> 30));
   };
   // requests of every unit; each thread has consecutive ones
@@ -309,26 +311,28 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   // more requests than pages cannot be met; sums stay within 32 bits that way
   if (mine > p.num_pages) { bad |= 2; mine = 0; }
   if (bad) atomicOr(&s.flag, bad);
-  int sum, ahead, need;
-  // (1024 threads x num_pages may pass 32 bits: the sum is formed in halves)
-  int sum_high;
-  const int my_low = static_cast<int>(mine & 0xffff), my_high = static_cast<int>(mine >> 16);
-  const int run_low = pg_scan(s, my_low, &sum), run_high = pg_scan(s, my_high, &sum_high);
-  const int64_t cta = static_cast<int64_t>(sum) + (static_cast<int64_t>(sum_high) << 16);
-  const bool too_many = cta > p.num_pages;
-  if (too_many && tid == 0) s.flag |= 2;
-  __syncthreads();
-  pg_cluster(s, too_many ? 0 : static_cast<int>(cta), &ahead, &need);
-  int flags = 0;
+  int64_t lo, hi;
+  pg_share(p.num_pages, rank, &lo, &hi);
+  const bool aligned = reinterpret_cast<uintptr_t>(p.to.refs) % 16 == 0;
+  PgFree free;
+  const int my_free = free.count(p.to.refs, aligned, lo, hi);
+  long long cta_need;
+  int cta_free;
+  const long long run_need = pg_scan<long long>(s, mine, &cta_need);
+  const int run_free = __shfl_sync(0xffffffffu, pg_scan<int>(s, (tid & 31) == 0 ? my_free : 0, &cta_free), 0);
+  if (tid == 0) {
+    if (cta_need > p.num_pages) s.flag |= 2;
+    s.block[0] = cta_need > p.num_pages ? 0 : static_cast<int>(cta_need);
+    s.block[1] = cta_free;
+  }
+  cluster.sync();
+  int ahead, need, place, free_all, flags = 0;
+  pg_cluster(s, 0, &ahead, &need);
+  pg_cluster(s, 1, &place, &free_all);
+  place += run_free;                       // the rank of this warp's first free page
 #pragma unroll
   for (int c = 0; c < kPgCluster; ++c) flags |= *cluster.map_shared_rank(&s.flag, c);
-  const bool aligned = reinterpret_cast<uintptr_t>(p.to.refs) % 16 == 0;
-  int64_t flo, fhi;
-  pg_share(p.num_pages, rank, &flo, &fhi);
-  const int my_free = pg_count_free(p.to.refs, aligned, flo, fhi);
-  int free_all;
-  int place = pg_ahead(s, my_free, &free_all);                   // the rank of this warp's first free page
-  const bool met = flags == 0 && static_cast<uint32_t>(need) <= static_cast<uint32_t>(free_all);
+  const bool met = flags == 0 && need <= free_all;               // (sums of eight shares of at most 2^27)
   if (rank == 0 && tid == 0) {
     p.state[0] = met ? 1 : 0;
     if (!met) atomicOr(p.status, (flags & 1 ? kStatusBadIndex : 0u) | ((flags & 2) || flags == 0 ? kStatusNoRoom : 0u));
@@ -336,11 +340,13 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   if (!met) {                              // the same in the whole cluster
     if (p.granted)
       for (int64_t u = u0; u < u1; ++u) p.granted[u] = 0;
+    cluster.sync();                        // nobody leaves while its sums are read
     return;
   }
-  for (int64_t base = flo; base < fhi && my_free && place < need; base += kPgTile) {       // (uniform over the warp)
+  int t = 0;
+  for (int64_t base = lo; base < hi && my_free && place < need; base += kPgTile, ++t) {    // (uniform over the warp)
     const int64_t i = base + (tid & 31) * 4;
-    const uint32_t bits = pg_free4(p.to.refs, aligned, i, fhi);
+    const uint32_t bits = free.tile(p.to.refs, aligned, i, hi, t);
     int total;
     int r = place + pg_lanes_ahead(__popc(bits), &total);
     place += total;
@@ -354,7 +360,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
         ++r;
       }
   }
-  int64_t off = ahead + static_cast<int64_t>(run_low) + (static_cast<int64_t>(run_high) << 16);
+  int64_t off = ahead + run_need;
   for (int64_t u = u0; u < u1; ++u) {
     const PgChild x = child(u);
     p.unit_off[u] = static_cast<int32_t>(off);
@@ -387,7 +393,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
       for (int j = lane; j < n; j += 32) to[j] = __ldcg(from + j);
     }
   }
-  cluster.sync();                          // lens of `from` may be those of `to`: they change behind everybody's last look
+  if (p.in_place) cluster.sync();          // lens of `from` are those of `to`: they change behind everybody's last look
   for (int64_t u = u0; u < u1; ++u) {
     const PgChild x = child(u);
     p.to.lens[u] = static_cast<int32_t>(x.rows_new);
@@ -423,25 +429,38 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_copy_kernel(const __gri
   const int32_t* src_table = p.from.tables + (static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads * p.max_pages + x.full;
   const int32_t* dst_table = p.to.tables + (static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads * p.max_pages + x.full;
   const int64_t page = static_cast<int64_t>(p.page_size) * p.row_pieces;
-  const int pieces = x.part * p.row_pieces;
-  for (int64_t i = threadIdx.x; i < static_cast<int64_t>(pieces) * p.num_kv_heads; i += kPgCarryThreads) {
-    const int64_t h = i / pieces, piece = i - h * pieces;
-    const int src = src_table[h * p.max_pages], dst = dst_table[h * p.max_pages];
+  const int64_t pieces = static_cast<int64_t>(x.part) * p.row_pieces;
+  const int lane = threadIdx.x & 31;
+  for (int h = threadIdx.x >> 5; h < p.num_kv_heads; h += kPgCarryThreads / 32) {          // a warp per head
+    const int src = src_table[static_cast<int64_t>(h) * p.max_pages], dst = dst_table[static_cast<int64_t>(h) * p.max_pages];
     if (src < 0 || src >= p.num_pages) {
-      if (piece == 0) atomicOr(p.status, kStatusBadPage);
+      if (lane == 0) atomicOr(p.status, kStatusBadPage);
       continue;
     }
-    const int64_t a = src * page + piece, b = dst * page + piece;
-    static_cast<uint4*>(p.k_pool)[b] = static_cast<const uint4*>(p.k_pool)[a];
-    static_cast<uint4*>(p.v_pool)[b] = static_cast<const uint4*>(p.v_pool)[a];
-  }
-  if (p.pos_pool)
-    for (int64_t i = threadIdx.x; i < static_cast<int64_t>(x.part) * p.num_kv_heads; i += kPgCarryThreads) {
-      const int64_t h = i / x.part, row = i - h * x.part;
-      const int src = src_table[h * p.max_pages], dst = dst_table[h * p.max_pages];
-      if (src < 0 || src >= p.num_pages) continue;
-      p.pos_pool[static_cast<int64_t>(dst) * p.page_size + row] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + row];
+    const uint4* ks = static_cast<const uint4*>(p.k_pool) + src * page;
+    const uint4* vs = static_cast<const uint4*>(p.v_pool) + src * page;
+    uint4* kd = static_cast<uint4*>(p.k_pool) + dst * page;
+    uint4* vd = static_cast<uint4*>(p.v_pool) + dst * page;
+    constexpr int kAhead = 4;
+    for (int64_t i = lane; i < pieces; i += 32 * kAhead) {
+      uint4 a[kAhead], b[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int64_t at = min(i + j * 32, pieces - 1);          // (the last piece again behind it)
+        a[j] = ks[at];
+        b[j] = vs[at];
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j * 32 < pieces) {
+          kd[i + j * 32] = a[j];
+          vd[i + j * 32] = b[j];
+        }
     }
+    if (p.pos_pool)
+      for (int i = lane; i < x.part; i += 32)
+        p.pos_pool[static_cast<int64_t>(dst) * p.page_size + i] = p.pos_pool[static_cast<int64_t>(src) * p.page_size + i];
+  }
 }
 
 // ------------------------------------------------------------------ compaction
@@ -458,24 +477,41 @@ __global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_con
   const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
   int64_t lo, hi;                          // this warp's pages
   pg_share(p.num_pages, rank, &lo, &hi);
-  const int free = pg_count_free(refs, aligned, lo, hi);
-  int all, moves;
-  pg_ahead(s, free, &all);
+  PgFree free;
+  const int mine = free.count(refs, aligned, lo, hi);
+  int cta, ahead, all;
+  const int run = __shfl_sync(0xffffffffu, pg_scan<int>(s, (tid & 31) == 0 ? mine : 0, &cta), 0);
+  if (tid == 0) s.block[0] = cta;
+  cluster.sync();
+  pg_cluster(s, 0, &ahead, &all);
+  ahead += run;                            // free pages ahead of this warp's
   const int used = p.num_pages - all;
-  // free pages below `used` and used ones from there on, ahead of this warp's; as many in all
-  const int64_t cut = min(max(static_cast<int64_t>(used), lo), hi);
-  const int holes = cut == hi ? free : (cut == lo ? 0 : pg_count_free(refs, aligned, lo, cut));
-  int mover = pg_ahead(s, static_cast<int>(hi - cut) - (free - holes), &moves), hole = pg_ahead(s, holes, &moves);
-  if (rank == 0 && tid == 0) {
-    p.state[0] = used;
-    p.state[1] = moves;
-    if (p.used) *p.used = used;
+  // The warp whose share the border lies in (the last one with pages, if that is the pool's end) counts the free pages below it.
+  if (lo <= used && (used < hi || (hi == p.num_pages && lo < hi))) {
+    int below = 0;
+    int t = 0;
+    for (int64_t base = lo; base < used; base += kPgTile, ++t) {
+      const int64_t i = base + (tid & 31) * 4;
+      const uint32_t in = i >= used ? 0u : (i + 4 <= used ? 15u : (1u << (used - i)) - 1u);
+      below += __popc(free.tile(refs, aligned, i, hi, t) & in);
+    }
+    below = __reduce_add_sync(0xffffffffu, below);
+    if ((tid & 31) == 0) {
+      p.state[0] = used;
+      p.state[1] = ahead + below;
+      if (p.used) *p.used = used;
+    }
   }
-  for (int64_t base = lo; base < hi; base += kPgTile) {
+  cluster.sync();
+  const int moves = __ldcg(p.state + 1);
+  int hole = ahead;                        // rank of this warp's first free page below the border,
+  int mover = static_cast<int>(max(static_cast<int64_t>(0), lo - used)) - max(0, ahead - moves);   // and of its first used one above
+  int t = 0;
+  for (int64_t base = lo; base < hi; base += kPgTile, ++t) {
     const int64_t i = base + (tid & 31) * 4;
-    const uint32_t free4 = pg_free4(refs, aligned, i, hi);
+    const uint32_t free4 = free.tile(refs, aligned, i, hi, t);
     const uint32_t there = i >= hi ? 0u : (i + 4 <= hi ? 15u : (1u << (hi - i)) - 1u);
-    const uint32_t below = i >= cut ? 0u : (i + 4 <= cut ? 15u : (1u << (cut - i)) - 1u);
+    const uint32_t below = i >= used ? 0u : (i + 4 <= used ? 15u : (1u << (used - i)) - 1u);
     const uint32_t hole4 = free4 & below, mover4 = there & ~below & ~free4;
     int total;
     int h = pg_lanes_ahead(__popc(hole4) | __popc(mover4) << 16, &total);
@@ -488,11 +524,22 @@ __global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_con
       const int32_t page = static_cast<int32_t>(i + e);
       if ((hole4 >> e) & 1u) p.list[h++] = page;
       if ((mover4 >> e) & 1u) p.second[m++] = page;
-      if ((free4 & ~below) >> e & 1u) p.place[page] = page;       // nothing should name it
+      if (((free4 & ~below) >> e) & 1u) p.place[page] = page;     // nothing should name it
     }
   }
   cluster.sync();                          // both lists are there
-  for (int m = rank * kPgThreads + tid; m < moves; m += kPgCluster * kPgThreads) p.place[__ldcg(p.second + m)] = __ldcg(p.list + m);
+  constexpr int kAhead = 4;
+  for (int m0 = rank * kPgThreads + tid; m0 < moves; m0 += kAhead * kPgCluster * kPgThreads) {
+    int from[kAhead], to[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int m = min(m0 + j * kPgCluster * kPgThreads, moves - 1);
+      from[j] = __ldcg(p.second + m);
+      to[j] = __ldcg(p.list + m);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) p.place[from[j]] = to[j];  // (the last one again behind it)
+  }
 }
 
 // Three independent jobs, each dealt out over the grid: pages to their new places, tables with the new places, refs of `to`.
