@@ -46,6 +46,7 @@ int cache_check(const pkv_config* c, const pkv_cache* x) {
 struct CacheWorkspace {
   uint32_t* status;
   int32_t* counters;
+  int32_t* group_counters;
   int32_t* state;
   float* partials;
   int32_t* unit_off;
@@ -69,6 +70,7 @@ CacheWorkspace carve_cache(const pkv_config* c, const pkv_cache* x, void* base) 
   w.state = static_cast<int32_t*>(take(256));
   // the counters, which have to be zero between calls, lie at the same place for every cache: a workspace may serve several
   w.counters = static_cast<int32_t*>(take(kMaxUnits * 4));
+  w.group_counters = static_cast<int32_t*>(take(size_t{2} * kCaMaxGrid * 4));
   w.partials = static_cast<float*>(take(size_t{2} * kCaMaxGrid * kCaPartial * sizeof(float)));
   w.unit_off = static_cast<int32_t*>(take(units * 4));
   w.list = static_cast<int32_t*>(take(pages * 4));
@@ -173,7 +175,6 @@ int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st)
   const int sms = device_sm_count();
   if (sms <= 0) return PKV_ERR_CUDA;
   const int64_t units = static_cast<int64_t>(p.batch) * p.num_kv_heads * p.head_blocks;
-  if (units <= 2 * sms) fit = std::min(fit, 2);                  // (see kCaPerSm)
   // no more CTAs than there can be tiles
   const int grid = static_cast<int>(std::min<int64_t>(std::min(kCaMaxGrid, sms * fit), (max_rows + kCaTile - 1) / kCaTile * units));
   launch_pdl(cache_attend_kernel<T, D, GT, POS>, dim3(grid), dim3(kCaThreads<T>), kSmem, st, p);
@@ -426,6 +427,7 @@ int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cac
   p.lse = lse_or_null;
   p.status = w.status;
   p.counters = w.counters;
+  p.group_counters = w.group_counters;
   p.partials = w.partials;
   p.batch = cache->batch;
   p.num_kv_heads = cfg->num_kv_heads;

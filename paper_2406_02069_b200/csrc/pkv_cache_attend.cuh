@@ -10,7 +10,8 @@
 //     sequence is split over many CTAs, and a CTA takes many short ones in turn, the next one's rows on their way while
 //     it finishes the one ahead.
 //   * A CTA that has all tiles of a head writes its output; otherwise it leaves (exponent, sum, weighted sum) in the workspace, and
-//     the last CTA of the head to arrive joins them in the order of the rows, so that equal calls give equal bits.
+//     the last CTA of the head to arrive joins them in the order of the rows (many of them in groups first), so that equal calls
+//     give equal bits.
 //   * A warp takes tiles of 16 rows, kStages of them in shared memory or on their way by asynchronous copies.  A row that is
 //     not seen is filled with zeros instead of read; a tile without a seen row costs its positions only.
 //   * 16-bit rows go through mma.sync, fp32 accumulation, the query heads as M: GT = 4 heads with the high, middle and low
@@ -34,11 +35,12 @@ template <typename T>
 constexpr int kCaThreads = kCaWarps<T> * 32;
 template <typename T>
 constexpr int kCaRows = kCaTile / kCaWarps<T>;
-// CTAs to an SM: three where there is a unit for each, two where units are split anyway and more parts only mean more to join
-// (131072 rows x 8 KV heads x 8 query heads: two 98 us, three 106; 64 sequences of 129 to 4096 rows, capped, window: 123 and 106).
+// CTAs to an SM: twelve warps hide more of a tile's chain of products, shuffles and exponentials than eight with all registers
+// (131072 rows x 8 KV heads x 8 query heads: two CTAs 114 us, three 102; 64 sequences of 129 to 4096 rows, capped, window: 123, 106).
 constexpr int kCaPerSm = 3;
 constexpr int kCaMaxGrid = kCaPerSm * 160; // CTAs at most (sizes the partial sums in the workspace)
 constexpr int kCaMaxHeads = 8;             // query heads of a CTA at most
+constexpr int kCaDirect = 32;              // parts of a unit that one CTA joins at once
 // Floats of one partial result: sums, then exponents, then weights' sums.
 constexpr int kCaPartial = kCaMaxHeads * (128 + 2);
 
@@ -57,6 +59,7 @@ struct CacheAttendParams {
   float* lse;                              // or null
   uint32_t* status;
   int32_t* counters;                       // [batch * H_kv * head_blocks], zero between calls
+  int32_t* group_counters;                 // [2 * gridDim.x], too
   float* partials;                         // [2 * gridDim.x][kCaPartial]
   int32_t batch, num_kv_heads, group, head_blocks;
   int32_t max_pages, page_size, num_pages;
@@ -468,27 +471,36 @@ __device__ __forceinline__ void ca_write(const CacheAttendParams& p, int64_t hea
   if (channel == 0 && p.lse) p.lse[head] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
 }
 
-// Partial results of a block of query heads -> its output, by one CTA.  The first one is at `first`, the others at rest + 2,
-// rest + 4 ... rest + 2 more.  The factors go to shared memory, to the last slots of the warps' rings in turn.  A warp finds the factors of a head; then every
-// thread has four channels of a head and adds up the partials in the order of the rows, kAhead loads on their way at a time.
-// (One channel and one load at a time: 120 us for the 37 partials of 8 heads x 128 channels, now 4.)
+// A unit's partial results: where they lie, in the order of its rows.
+struct CaParts {
+  int first, rest, count;                  // the first one, then rest + 2, rest + 4 ..
+  __device__ __forceinline__ int at(int i) const { return i == 0 ? first : rest + 2 * i; }
+  // More than kCaDirect are joined in groups first, each by its own last CTA: the parts of a group, and of the unit's joined groups.
+  __device__ __forceinline__ int group() const { return count <= kCaDirect ? count : static_cast<int>(ceilf(sqrtf(static_cast<float>(count)))); }
+};
+
+// Parts i0, i0 + stride .. (count of them) of a unit -> its output, or (part) one partial result that takes the place of the
+// first.  By one CTA.  The factors go to shared memory, to the last slots of the warps' rings in turn.  A warp finds the factors
+// of a head; then every thread has four channels of a head and adds up the parts in the order of the rows, kAhead loads on their
+// way at a time.  (One channel and one load at a time: 120 us for the 37 parts of 8 heads x 128 channels; 55 of them 20 us this
+// way; 131072 rows x 8 KV heads x 8 query heads in all 102 us, in groups 98.)
 template <typename T, int D, int GT>
-__device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* last_slots, uint32_t ring, int first, int more, int rest, int heads,
-                                        int64_t head0) {
+__device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* last_slots, uint32_t ring, const CaParts& parts, int i0, int stride,
+                                        int count, int heads, int64_t head0, bool part) {
   constexpr int kAhead = 8;
   __shared__ float s_jm[GT], s_jz[GT];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   auto factor = [&](int i) -> float* { return reinterpret_cast<float*>(last_slots + (i % kCaWarps<T>) * ring) + i / kCaWarps<T> * GT; };
-  auto partial = [&](int i) { return p.partials + static_cast<int64_t>(i == 0 ? first : rest + 2 * i) * kCaPartial; };
+  auto partial = [&](int i) { return p.partials + static_cast<int64_t>(parts.at(i0 + i * stride)) * kCaPartial; };
   float4 x[kAhead];
   auto fetch = [&](int i, int o) {         // (the last one again behind it: loads without a condition go out together)
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) x[j] = __ldcg(reinterpret_cast<const float4*>(partial(min(i + j, more)) + o));
+    for (int j = 0; j < kAhead; ++j) x[j] = __ldcg(reinterpret_cast<const float4*>(partial(min(i + j, count - 1)) + o));
   };
   fetch(0, min(static_cast<int>(threadIdx.x) * 4, heads * D - 4));               // on their way while the factors are found
   for (int g = warp; g < heads; g += kCaWarps<T>) {
     float m = -INFINITY, z0 = 0.f;
-    for (int i = lane; i <= more; i += 32) {
+    for (int i = lane; i < count; i += 32) {
       const float mi = __ldcg(partial(i) + GT * D + g);
       if (i == lane) z0 = __ldcg(partial(i) + GT * D + GT + g);
       factor(i)[g] = mi;
@@ -497,7 +509,7 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
     float z = 0.f;
-    for (int i = lane; i <= more; i += 32) {
+    for (int i = lane; i < count; i += 32) {
       const float f = ca_factor(factor(i)[g], m);
       factor(i)[g] = f;
       z = fmaf(i == lane ? z0 : __ldcg(partial(i) + GT * D + GT + g), f, z);
@@ -513,11 +525,11 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
   for (int o = threadIdx.x * 4; o < heads * D; o += kCaThreads<T> * 4) {
     const int g = o / D;
     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i <= more; i += kAhead) {
+    for (int i = 0; i < count; i += kAhead) {
       if (i > 0 || o >= kCaThreads<T> * 4) fetch(i, o);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (i + j <= more) {
+        if (i + j < count) {
           const float f = factor(i + j)[g];
           a.x = fmaf(x[j].x, f, a.x);
           a.y = fmaf(x[j].y, f, a.y);
@@ -526,13 +538,35 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
         }
       }
     }
-    const float m = s_jm[g], z = s_jz[g];
-    const int channel = o - g * D;
-    ca_write(p, head0 + g, D, channel, m, z, a.x);
-    ca_write(p, head0 + g, D, channel + 1, m, z, a.y);
-    ca_write(p, head0 + g, D, channel + 2, m, z, a.z);
-    ca_write(p, head0 + g, D, channel + 3, m, z, a.w);
+    if (part) {
+      __stcg(reinterpret_cast<float4*>(partial(0) + o), a);
+    } else {
+      const float m = s_jm[g], z = s_jz[g];
+      const int channel = o - g * D;
+      ca_write(p, head0 + g, D, channel, m, z, a.x);
+      ca_write(p, head0 + g, D, channel + 1, m, z, a.y);
+      ca_write(p, head0 + g, D, channel + 2, m, z, a.z);
+      ca_write(p, head0 + g, D, channel + 3, m, z, a.w);
+    }
   }
+  if (part && threadIdx.x < heads) {
+    __stcg(partial(0) + GT * D + threadIdx.x, s_jm[threadIdx.x]);
+    __stcg(partial(0) + GT * D + GT + threadIdx.x, s_jz[threadIdx.x]);
+  }
+}
+
+// Whether this CTA is the last of `of` to arrive at a counter, which is zero again then.  Everything that the CTA wrote ahead is
+// there for the last one to read.
+__device__ __forceinline__ bool ca_last(int32_t* counter, int of, int32_t* s_last) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();                       // for the whole CTA, which the barrier has ordered before it
+    *s_last = atomicAdd(counter, 1) == of - 1;
+    if (*s_last) *counter = 0;             // everybody has arrived: ready for the next call
+    __threadfence();
+  }
+  __syncthreads();
+  return *s_last != 0;
 }
 
 // How the tiles of a call are dealt out.  A unit is a block of query heads of one KV head of one sequence; s_off has the tiles of
@@ -545,6 +579,9 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
 // 14.6 us in equal ranges, where nearly every CTA has the end of one unit and the start of another.)
 constexpr int kCaStart = 2;
 constexpr int kCaSpare = 3;                // tiles that parts may have more than equal ranges would
+// A split has to save so many tiles in turn: handing sums over and joining them takes 2.8 us, a tile about 1 (128 rows of one
+// sequence, 8 KV heads: 8.8 us in two parts, 7.4 in one; 512 rows: 9.2 in eight, 10.0 in four, 11.5 in two).
+constexpr int kCaSplit = 3;
 
 struct CaSegment {
   int b, unit;                             // sequence (-1: no segment) and unit of it: KV head * head_blocks + block
@@ -627,7 +664,12 @@ __device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq,
       if (parts(mid) <= ctas) hi = mid;
       else lo = mid + 1;
     }
-    if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) most = static_cast<int>(hi);
+    if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) {
+      int longest = 0;
+      for (int s = lane; s < batch; s += 32) longest = max(longest, off[s + 1] - off[s]);
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      most = longest < static_cast<int>(hi) + kCaSplit ? longest : static_cast<int>(hi);
+    }
   }
   __syncwarp();
   if (most == 0) {
@@ -861,16 +903,19 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
       }
     }
     if (!was.whole) {
-      __syncthreads();
-      if (tid == 0) {
-        __threadfence();                   // for the whole CTA, which the barrier has ordered before it
-        int32_t* counter = p.counters + static_cast<int64_t>(was.b) * s_plan.per_seq + was.unit;
-        s_last = atomicAdd(counter, 1) == was.more;
-        if (s_last) *counter = 0;          // everybody has arrived: ready for the next call
-        __threadfence();
+      const CaParts parts{was.first, was.rest, was.more + 1};
+      const int group = parts.group(), groups = (parts.count + group - 1) / group;
+      const int mine = was.slot == was.first ? 0 : (was.slot - was.rest) / 2, i0 = mine / group * group;
+      const uint32_t ring_bytes = static_cast<uint32_t>(W::kRing);
+      int32_t* unit_counter = p.counters + static_cast<int64_t>(was.b) * s_plan.per_seq + was.unit;
+      if (groups == 1) {
+        if (ca_last(unit_counter, parts.count, &s_last))
+          ca_join<T, D, GT>(p, ca_smem + kAcc, ring_bytes, parts, 0, 1, parts.count, heads_was, head0, false);
+      } else if (ca_last(p.group_counters + parts.at(i0), min(group, parts.count - i0), &s_last)) {
+        ca_join<T, D, GT>(p, ca_smem + kAcc, ring_bytes, parts, i0, 1, min(group, parts.count - i0), heads_was, head0, true);
+        if (ca_last(unit_counter, groups, &s_last))
+          ca_join<T, D, GT>(p, ca_smem + kAcc, ring_bytes, parts, 0, group, groups, heads_was, head0, false);
       }
-      __syncthreads();
-      if (s_last) ca_join<T, D, GT>(p, ca_smem + kAcc, static_cast<uint32_t>(W::kRing), was.first, was.more, was.rest, heads_was, head0);
     }
     if (!have) return;
     __syncthreads();                       // the sums have been read: the last slot may be filled
