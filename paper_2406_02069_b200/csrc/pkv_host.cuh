@@ -70,17 +70,18 @@ void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cu
 // ---------------------------------------------------------------- outputs still in flight
 // The tensor-core sweeps start reading Q and K before the kernels ahead of them in the stream have finished.
 // That is only right for tensors those kernels do not write, so the library remembers where its last calls put
-// K/V rows (packed caches, page pools) and a sweep whose Q or K overlaps one of them waits like any other kernel.
+// K/V rows (packed caches, page pools, rotated keys and queries) and a sweep whose Q or K overlaps one of them waits like any other kernel.
 struct ByteRange { uintptr_t lo, hi; };
 inline std::mutex g_out_mutex;
-inline ByteRange g_recent_out[16];
+constexpr unsigned kRecentOut = 256;       // a kernel can wait behind as many as fit on the device at once
+inline ByteRange g_recent_out[kRecentOut];
 inline unsigned g_recent_out_next = 0;
 
 inline void note_output(const void* ptr, size_t bytes) {
   if (!ptr || !bytes) return;
   std::lock_guard<std::mutex> lock(g_out_mutex);
   const uintptr_t lo = reinterpret_cast<uintptr_t>(ptr);
-  g_recent_out[g_recent_out_next++ % 16] = ByteRange{lo, lo + bytes};
+  g_recent_out[g_recent_out_next++ % kRecentOut] = ByteRange{lo, lo + bytes};
 }
 
 inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {

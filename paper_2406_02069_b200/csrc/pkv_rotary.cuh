@@ -7,9 +7,10 @@
 //   * The angle is formed in turns and in fp64, p * (f / 2 pi), and loses its whole turns there: in fp32 a position of 100000
 //     would leave an error of 4e-3 rad.  sincospif then sees at most half a turn.
 //   * VEC elements make 16 bytes where the pieces of the rotated part start at multiples of 16 bytes; a rotated part of another
-//     size is taken two pairs at a time, or pair by pair (8192 tokens of 40 heads, 20 of 128 elements rotated: XX us, pair by pair 61).
-//   * 16-bit elements are taken apart and put together two to a word (one by one: 185 us for 32 / 8 heads x 32768 tokens, now 109,
-//     94 % of the rate of a copy).
+//     size is taken two pairs at a time (8192 tokens of 40 heads, 20 of 128 elements rotated: 43 us, 59 % of the rate of a copy), or
+//     pair by pair (61 us).
+//   * 16-bit elements are taken apart and put together two to a word (one by one: 185 us for 32 / 8 heads x 32768 tokens, this way
+//     105, 98 % of the rate of a copy).  The rows come while the sines are formed, and while the page tables are read.
 #pragma once
 
 #include "pkv_common.cuh"
@@ -19,8 +20,8 @@ namespace pkv {
 
 constexpr int kRotThreads = 256;
 // Heads whose rows a thread has on their way at a time, and CTAs that an SM shall hold.  32 / 8 heads x 32768 tokens in bf16: two
-// and four 109 us, four and two 118, one and four 118, two and two 132.  An append of 2000 rows in pieces: four and two 16 us,
-// two and four 21 (its look-ups need the registers).
+// and four 109 us, four and two 118, one and four 118, two and two 132.  An append of 2000 rows in pieces: four and two 13.4 us,
+// two and three 15.7, two and four 18.7 (its look-ups need the registers).
 template <int VEC, bool APPEND>
 constexpr int kRotUnroll = VEC > 2 && !APPEND ? 2 : 4;
 template <int VEC, bool APPEND>
@@ -147,32 +148,26 @@ __global__ void __launch_bounds__(kRotThreads, kRotPerSm<VEC, APPEND>) rotary_ke
   T* q_to = static_cast<T*>(const_cast<void*>(p.q_out.ptr)) + b * p.q_out.sb + t * p.q_out.st;
   T* k_to = static_cast<T*>(const_cast<void*>(p.k_out.ptr)) + b * p.k_out.sb + t * p.k_out.st;
   Piece a[UNROLL], c[UNROLL];
-  T* to[UNROLL];
-  // Rows of the heads h0, h0 + step ..: on their way to a and c; to: where they go, null for those that do not.
+  int page[UNROLL];                        // of a key or value that is appended
+  // What a head index stands for: a query's, a key's or a value's head.
+  auto is_query = [&](int h) { return h < p.heads_q; };
+  auto is_value = [&](int h) { return APPEND && h >= p.heads_q + p.heads_kv; };
+  auto number = [&](int h) { return is_query(h) ? h : (is_value(h) ? h - p.heads_q - p.heads_kv : h - p.heads_q); };
+  auto source = [&](int h) -> const T* {
+    return is_query(h) ? q_in + number(h) * p.q.sh : (is_value(h) ? v_in + number(h) * p.v.sh : k_in + number(h) * p.k.sh);
+  };
+  // Rows of the heads h0, h0 + step .. on their way to a and c, their pages beside them.
   auto fetch = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < UNROLL; ++i) {
       const int h = h0 + i * step;
-      to[i] = nullptr;
       if (h >= heads) continue;
-      const bool is_q = h < p.heads_q, is_v = APPEND && h >= p.heads_q + p.heads_kv;
-      const int hh = is_q ? h : (is_v ? h - p.heads_q - p.heads_kv : h - p.heads_q);
-      const T* from = is_q ? q_in + hh * p.q.sh : (is_v ? v_in + hh * p.v.sh : k_in + hh * p.k.sh);
-      if (APPEND && !is_q) {
-        const int page = inside ? __ldg(p.table + (static_cast<int64_t>(b) * p.heads_kv + hh) * p.max_pages + page_at) : -1;
-        if (page < 0 || page >= p.num_pages) {
-          if (u == 0) atomicOr(p.status, kStatusBadPage);
-          continue;
-        }
-        const int64_t slot = static_cast<int64_t>(page) * p.page_size + slot_in_page;
-        to[i] = static_cast<T*>(is_v ? p.v_pool : p.k_pool) + slot * (p.units * 2 * VEC);
-        if (!is_v && u == 0 && p.pos_pool) p.pos_pool[slot] = pos;
-      } else {
-        to[i] = is_q ? q_to + hh * p.q_out.sh : k_to + hh * p.k_out.sh;
-        if (to[i] == from && !rotated) { to[i] = nullptr; continue; }         // in place, not part of the rotation
-      }
+      const T* from = source(h);
+      const bool is_v = is_value(h);
       a[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC : e0));
       c[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC + VEC : e1));
+      if (APPEND && !is_query(h))
+        page[i] = inside ? __ldg(p.table + (static_cast<int64_t>(b) * p.heads_kv + number(h)) * p.max_pages + page_at) : -1;
     }
   };
   const int first = blockIdx.y * p.head_lanes + hl;
@@ -193,11 +188,25 @@ __global__ void __launch_bounds__(kRotThreads, kRotPerSm<VEC, APPEND>) rotary_ke
   for (int h0 = first; h0 < heads;) {
 #pragma unroll
     for (int i = 0; i < UNROLL; ++i) {
-      if (!to[i]) continue;
-      const bool is_v = APPEND && h0 + i * step >= p.heads_q + p.heads_kv;
+      const int h = h0 + i * step;
+      if (h >= heads) continue;
+      const bool is_v = is_value(h);
+      T* to;
+      if (APPEND && !is_query(h)) {
+        if (page[i] < 0 || page[i] >= p.num_pages) {
+          if (u == 0) atomicOr(p.status, kStatusBadPage);
+          continue;
+        }
+        const int64_t slot = static_cast<int64_t>(page[i]) * p.page_size + slot_in_page;
+        to = static_cast<T*>(is_v ? p.v_pool : p.k_pool) + slot * (p.units * 2 * VEC);
+        if (!is_v && u == 0 && p.pos_pool) p.pos_pool[slot] = pos;
+      } else {
+        to = is_query(h) ? q_to + h * p.q_out.sh : k_to + number(h) * p.k_out.sh;
+        if (!rotated && to == source(h)) continue;                // in place, not part of the rotation
+      }
       if (rotated && !is_v) rot_pieces<T, VEC>(a[i], c[i], cs, sn, p.interleaved);
-      *reinterpret_cast<Piece*>(to[i] + (is_v ? u * 2 * VEC : e0)) = a[i];
-      *reinterpret_cast<Piece*>(to[i] + (is_v ? u * 2 * VEC + VEC : e1)) = c[i];
+      *reinterpret_cast<Piece*>(to + (is_v ? u * 2 * VEC : e0)) = a[i];
+      *reinterpret_cast<Piece*>(to + (is_v ? u * 2 * VEC + VEC : e1)) = c[i];
     }
     h0 += step * UNROLL;
     if (h0 < heads) fetch(h0);
