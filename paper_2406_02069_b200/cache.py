@@ -60,6 +60,10 @@ def make_rotary(rotary_dim: int, *, layout: str = "half", base: float = 10000.0,
     return plan
 
 
+def _plan(plan: PkvRotary) -> None:
+    _want(isinstance(plan, PkvRotary), "a plan of rotary positions is what make_rotary gives")
+
+
 def _same_device(tensors) -> None:
     """The library launches on the current device: the tensors have to be its."""
     current = torch.cuda.current_device()
@@ -167,6 +171,7 @@ def rotary(cfg: PkvConfig, plan: PkvRotary, positions: torch.Tensor, q: Optional
     if st != _NOT_TAKEN:
         _check(st, "pyramidkv_rotary")
         return
+    _plan(plan)
     _want(q is not None or k is not None, "rotary needs q or k")
     _want((q is not None or q_out is None) and (k is not None or k_out is None), "an output without its input")
     q_out, k_out = (q if q_out is None else q_out), (k if k_out is None else k_out)
@@ -202,6 +207,8 @@ def append_cache(cfg: PkvConfig, cache: PagedCache, layer: int, positions: Optio
     if q is not None:
         _rows(cfg, "q", q, cache.batch, cfg.num_q_heads, tokens)
         _rows(cfg, "q_out", q_out, cache.batch, cfg.num_q_heads, tokens)
+    if rotary is not None:
+        _plan(rotary)
     _want(positions is not None or (rotary is None and cache.positions is None), "positions are needed for the rotation and for the cache's positions")
     stride = _positions(positions, cache.batch, tokens) if positions is not None else 0
     if counts is not None:

@@ -444,6 +444,7 @@ int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cac
   const double log2e = 1.4426950408889634, scale = o.scale == 0.f ? 1.0 / std::sqrt(static_cast<double>(cfg->head_dim)) : o.scale;
   p.cap_log2 = static_cast<float>(o.softcap * log2e);
   p.scale_log2 = static_cast<float>(o.softcap > 0.f ? scale / o.softcap : scale * log2e);
+  if (!std::isfinite(p.cap_log2) || !std::isfinite(p.scale_log2)) return PKV_ERR_INVALID_ARG;  // a cap too close to zero for fp32
   const int gt = heads_per_cta(cfg);
   const bool wide = cfg->head_dim == 128;
   const int64_t rows = static_cast<int64_t>(cache->max_pages) * cache->page_size;

@@ -163,7 +163,7 @@ def test_rotations_that_make_no_sense_are_refused(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(layer=2), dict(out=None), dict(out=P + 2), dict(lse=P + 1), dict(q=NONE), dict(q=tensor(ptr=P + 2)),
-                                dict(q=tensor(sh=68)), dict(scale=math.nan), dict(softcap=-1.0), dict(softcap=math.inf), dict(window=-1, q_positions=P),
+                                dict(q=tensor(sh=68)), dict(scale=math.nan), dict(softcap=-1.0), dict(softcap=math.inf), dict(softcap=1e-40), dict(window=-1, q_positions=P),
                                 dict(window=5), dict(prefix=1), dict(slopes=P), dict(slopes=P + 1, q_positions=P), dict(q_positions=P + 2),
                                 dict(q_positions=P, c=cache(positions=None))], ids=lambda kw: "_".join(kw))
 def test_attention_that_makes_no_sense_is_refused(kw):

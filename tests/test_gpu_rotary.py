@@ -271,3 +271,6 @@ def test_tensors_that_do_not_fit_are_refused():
             pkv.rotary(cfg, plan, p, bad["q"], bad["k"], bad.get("q_out"))
     with pytest.raises(ValueError):
         pkv.append_cache(config((4, 2), 64, "fp16"), cache, 0, p, k, k, ws)      # another configuration's cache
+    for call in (lambda: pkv.rotary(cfg, None, p, q), lambda: pkv.append_cache(cfg, cache, 0, p, k, k, ws, rotary=128)):
+        with pytest.raises(ValueError):                              # no plan
+            call()
