@@ -36,7 +36,8 @@ int cache_check(const pkv_config* c, const pkv_cache* x) {
   if ((x->positions && !pointer_ok(x->positions, 4)) || (x->refs && !pointer_ok(x->refs, 4))) return PKV_ERR_INVALID_ARG;
   if (x->num_pages < 1 || x->page_size < 1 || x->layers < 1 || x->batch < 1 || x->max_pages < 1) return PKV_ERR_INVALID_ARG;
   const int64_t rows = static_cast<int64_t>(x->max_pages) * x->page_size;
-  if (x->batch > PKV_MAX_CACHE_BATCH || x->layers > 65535 || c->num_kv_heads > 65535 || x->num_pages > kMaxPages || rows > kMaxRows)
+  if (x->batch > PKV_MAX_CACHE_BATCH || x->layers > 65535 || c->num_kv_heads > 65535 || x->num_pages > kMaxPages || rows > kMaxRows ||
+      static_cast<int64_t>(x->num_pages) * x->page_size > INT32_MAX)
     return PKV_ERR_UNSUPPORTED;
   if ((rows + kCaTile - 1) / kCaTile * x->batch > INT32_MAX) return PKV_ERR_UNSUPPORTED;      // tiles of a head
   if (static_cast<int64_t>(x->batch) * c->num_kv_heads * head_blocks(c) > kMaxUnits) return PKV_ERR_UNSUPPORTED;

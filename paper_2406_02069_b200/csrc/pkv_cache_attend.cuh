@@ -85,9 +85,9 @@ struct CaRows {
   int32_t q_pos;
 };
 
-// Row r's place in the pool, counted in rows; -1 if it has none.
+// Row r's place in the pool, counted in rows (the host keeps those below 2^31); -1 if it has none.
 template <int POS>
-__device__ __forceinline__ int64_t ca_place(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report) {
+__device__ __forceinline__ int ca_place(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report) {
   if (r >= s.rows) return -1;
   const int j = p.page_shift >= 0 ? r >> p.page_shift : r / p.page_size;
   const int page = __ldg(s.table + j);
@@ -95,7 +95,7 @@ __device__ __forceinline__ int64_t ca_place(const CacheAttendParams& p, const Ca
     if (report) atomicOr(p.status, kStatusBadPage);
     return -1;
   }
-  return static_cast<int64_t>(page) * p.page_size + (r - j * p.page_size);
+  return page * p.page_size + (r - j * p.page_size);
 }
 
 // Whether the row at a place is seen, by its position; *far: p - p_r.
@@ -123,10 +123,10 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
 #pragma unroll 1
     for (int r = t0; r < min(t0 + kCaRows<T>, s.rows); ++r) {
       uint32_t far = 0;
-      const int64_t at = ca_place<POS>(p, s, r, false);
+      const int at = ca_place<POS>(p, s, r, false);
       if (at < 0 || (POS && !ca_seen<POS>(p, s, __ldg(p.pos_pool + at), &far))) continue;
-      const T* k = static_cast<const T*>(p.k_pool) + at * D + lane * PER;
-      const T* v = static_cast<const T*>(p.v_pool) + at * D + lane * PER;
+      const T* k = static_cast<const T*>(p.k_pool) + static_cast<int64_t>(at) * D + lane * PER;
+      const T* v = static_cast<const T*>(p.v_pool) + static_cast<int64_t>(at) * D + lane * PER;
       float dot = 0.f;
 #pragma unroll
       for (int c = 0; c < PER; ++c) dot = fmaf(qv[c], to_float(k[c]), dot);
@@ -161,13 +161,13 @@ struct CaWarp {
     return (piece ^ (((r >> 1) & 3) << 1)) << 4;
   }
 
-  __device__ __forceinline__ static void copy_tile(const CacheAttendParams& p, uint32_t to_tile, int64_t mine) {
+  __device__ __forceinline__ static void copy_tile(const CacheAttendParams& p, uint32_t to_tile, int mine) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int s = 0; s < TR / ROWS_AT_ONCE; ++s) {
       const int r = s * ROWS_AT_ONCE + lane / PIECES, piece = lane % PIECES;
-      const int64_t at = __shfl_sync(0xffffffffu, mine, r);
-      const int64_t from = (at >= 0 ? at : 0) * D + piece * (16 / static_cast<int>(sizeof(T)));
+      const int at = __shfl_sync(0xffffffffu, mine, r);
+      const int64_t from = static_cast<int64_t>(max(at, 0)) * D + piece * (16 / static_cast<int>(sizeof(T)));
       const uint32_t to = to_tile + r * ROW;
       dec_copy16(to + k_place(r, piece), static_cast<const T*>(p.k_pool) + from, at >= 0);
       dec_copy16(to + TILE + v_place(r, piece), static_cast<const T*>(p.v_pool) + from, at >= 0);
@@ -205,8 +205,7 @@ struct CaSums {
   // seen: bit r for row r of the tile; far: lane r (and r + 16) has row r's distance.
   __device__ __forceinline__ void step(const CacheAttendParams& p, uint32_t k_at, uint32_t v_at, uint32_t seen, uint32_t far) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    float x[2][2];
-    float mx = -INFINITY;
+    float x[2][2], mx;
     float s0[2][4], s1[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -222,17 +221,28 @@ struct CaSums {
         X::mma(s1[t], qj.z, qj.z, qj.w, qj.w, k.z, k.w);
       }
     }
+    auto logit = [&](int t, int i) {
+      const int r = t * 8 + 2 * c + i;
+      float d = 0.f;
+      if (POS == 2) d = __uint2float_rn(__shfl_sync(0xffffffffu, far, r));
+      const float dot = t == 0 ? s0[0][i] + s1[0][i] : s0[1][i] + s1[1][i];
+      return (seen >> r) & 1u ? ca_logit<POS>(p, dot, slope, d) : -INFINITY;
+    };
+    if (GT == 4 && p.cap_log2 != 0.f) {    // lanes g and g + 4 have the same dot products: each caps half of them
+      const bool upper = g >= 4;
+      const float y0 = logit(upper, 0), y1 = logit(upper, 1);
+      const float o0 = __shfl_xor_sync(0xffffffffu, y0, 16), o1 = __shfl_xor_sync(0xffffffffu, y1, 16);
+      x[0][0] = upper ? o0 : y0;
+      x[0][1] = upper ? o1 : y1;
+      x[1][0] = upper ? y0 : o0;
+      x[1][1] = upper ? y1 : o1;
+    } else {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int r = t * 8 + 2 * c + i;
-        float d = 0.f;
-        if (POS == 2) d = __uint2float_rn(__shfl_sync(0xffffffffu, far, r));
-        x[t][i] = (seen >> r) & 1u ? ca_logit<POS>(p, s0[t][i] + s1[t][i], slope, d) : -INFINITY;
-        mx = fmaxf(mx, x[t][i]);
-      }
+        for (int i = 0; i < 2; ++i) x[t][i] = logit(t, i);
     }
+    mx = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
     const float mn = fmaxf(m, mx);
@@ -781,19 +791,19 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
   const T* q0;
   int first, heads, which = 0;
   uint32_t seen[kCaStages], far[kCaStages];                      // of the tiles in the ring, oldest first
-  int64_t mine_last, next;                                       // where the rows of the last slot's tile lie, and the next one's
+  int mine_last, next;                                           // where the rows of the last slot's tile lie, and the next one's
   int next_pos;
   int q_buffer = 0;
   Sums sums;
   // Rows are looked up in two steps, a tile apart: a row's place, then its position.  Lane l has row l % TR.
   auto place = [&](int t0) { return ca_place<POS>(p, rows, t0 + lane % W::TR, lane < W::TR); };
-  auto position = [&](int64_t at) { return POS && at >= 0 ? __ldg(p.pos_pool + at) : 0; };
-  auto judge = [&](int64_t at, int pos, uint32_t* f) -> int64_t {                  // the place, -1 if the row is not seen
+  auto position = [&](int at) { return POS && at >= 0 ? __ldg(p.pos_pool + at) : 0; };
+  auto judge = [&](int at, int pos, uint32_t* f) -> int {                          // the place, -1 if the row is not seen
     *f = 0;
     return POS && at >= 0 && !ca_seen<POS>(p, rows, pos, f) ? -1 : at;
   };
   constexpr uint32_t kRowBits = W::TR == 32 ? 0xffffffffu : (1u << W::TR) - 1u;
-  auto copy_in = [&](uint32_t slot, uint32_t there, int64_t mine) {
+  auto copy_in = [&](uint32_t slot, uint32_t there, int mine) {
     if (there) W::copy_tile(p, ring + slot, mine);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -807,7 +817,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     rows.rows = min(min(max(__ldg(p.lens + seg.b), 0), most), seg.tile1 * kCaTile);
     rows.q_pos = POS ? __ldg(p.q_pos + seg.b) : 0;
     first = seg.tile0 * kCaTile + warp * W::TR;
-    int64_t mine[kCaStages];
+    int mine[kCaStages];
     int pos[kCaStages];
 #pragma unroll
     for (int s = 0; s < kCaStages; ++s) mine[s] = place(first + s * kCaTile);
@@ -844,7 +854,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     copy_in(kAcc, seen[kCaStages - 1], mine_last);
     const int next_seg = which == 2 ? 0 : which + 1;
     if (tid == THREADS - 1) ca_next(s_off, &s_plan, &s_seg[3 - which - next_seg]);       // (while the rows come)
-    int64_t second = place(first + (kCaStages + 1) * kCaTile);   // one tile further
+    int second = place(first + (kCaStages + 1) * kCaTile);   // one tile further
 
     // ---- the warp's rows
     uint32_t slot = 0;
@@ -858,7 +868,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
         seen[s] = seen[s + 1];
         far[s] = far[s + 1];
       }
-      const int64_t mine = judge(next, next_pos, &far[kCaStages - 1]);
+      const int mine = judge(next, next_pos, &far[kCaStages - 1]);
       seen[kCaStages - 1] = __ballot_sync(0xffffffffu, mine >= 0) & kRowBits;
       copy_in(slot, seen[kCaStages - 1], mine);
       next = second;

@@ -107,7 +107,7 @@ def compact(c=None, to=None, used=None, ws=P, size=BIG):
 BAD_CACHES = [(dict(k_pool=None), INVALID), (dict(v_pool=P + 8), INVALID), (dict(tables=None), INVALID), (dict(lens=P + 2), INVALID),
               (dict(positions=P + 1), INVALID), (dict(refs=P + 3), INVALID), (dict(num_pages=0), INVALID), (dict(page_size=0), INVALID),
               (dict(layers=0), INVALID), (dict(batch=0), INVALID), (dict(max_pages=-1), INVALID), (dict(batch=1025), UNSUPPORTED),
-              (dict(layers=65536), UNSUPPORTED), (dict(num_pages=(1 << 27) + 1), UNSUPPORTED), (dict(max_pages=1 << 20, page_size=1025), UNSUPPORTED),
+              (dict(layers=65536), UNSUPPORTED), (dict(num_pages=(1 << 27) + 1), UNSUPPORTED), (dict(num_pages=1 << 27, page_size=16), UNSUPPORTED), (dict(max_pages=1 << 20, page_size=1025), UNSUPPORTED),
               (dict(max_pages=1 << 30, page_size=1, batch=512), UNSUPPORTED)]
 
 
