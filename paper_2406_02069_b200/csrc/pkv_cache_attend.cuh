@@ -90,7 +90,7 @@ template <int POS>
 __device__ __forceinline__ int ca_place(const CacheAttendParams& p, const CaRows<POS>& s, int r, bool report) {
   if (r >= s.rows) return -1;
   const int j = p.page_shift >= 0 ? r >> p.page_shift : r / p.page_size;
-  const int page = __ldg(s.table + j);
+  const int page = s.table[j];
   if (page < 0 || page >= p.num_pages) {
     if (report) atomicOr(p.status, kStatusBadPage);
     return -1;
@@ -124,7 +124,7 @@ __device__ __noinline__ void ca_sum_special(const CacheAttendParams& p, const Ca
     for (int r = t0; r < min(t0 + kCaRows<T>, s.rows); ++r) {
       uint32_t far = 0;
       const int at = ca_place<POS>(p, s, r, false);
-      if (at < 0 || (POS && !ca_seen<POS>(p, s, __ldg(p.pos_pool + at), &far))) continue;
+      if (at < 0 || (POS && !ca_seen<POS>(p, s, p.pos_pool[at], &far))) continue;
       const T* k = static_cast<const T*>(p.k_pool) + static_cast<int64_t>(at) * D + lane * PER;
       const T* v = static_cast<const T*>(p.v_pool) + static_cast<int64_t>(at) * D + lane * PER;
       float dot = 0.f;
@@ -195,7 +195,7 @@ struct CaSums {
     const int lane = threadIdx.x & 31, g = (lane >> 2) % GT, c = lane & 3;
     const bool there = g < heads;
     q = q_shared + g * kQ + c * 16;
-    slope = POS == 2 && there ? __ldg(p.slopes + hq + g) * 1.4426950408889634f : 0.f;
+    slope = POS == 2 && there ? p.slopes[hq + g] * 1.4426950408889634f : 0.f;
 #pragma unroll
     for (int i = 0; i < VC * 8; ++i) o[i][0] = o[i][1] = 0ull;
     m = -INFINITY;
@@ -748,7 +748,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
   pdl_wait();
 
   // ---- tiles of every sequence and their running sum
-  auto tiles_of = [&](int b) { return max(1, (min(max(__ldg(p.lens + b), 0), most) + kCaTile - 1) / kCaTile); };
+  auto tiles_of = [&](int b) { return max(1, (min(max(p.lens[b], 0), most) + kCaTile - 1) / kCaTile); };
   if (p.batch <= 32) {                     // every warp for itself: all write the same
     const int x = lane < p.batch ? tiles_of(lane) : 0;
     int run = x;
@@ -797,7 +797,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
   Sums sums;
   // Rows are looked up in two steps, a tile apart: a row's place, then its position.  Lane l has row l % TR.
   auto place = [&](int t0) { return ca_place<POS>(p, rows, t0 + lane % W::TR, lane < W::TR); };
-  auto position = [&](int at) { return POS && at >= 0 ? __ldg(p.pos_pool + at) : 0; };
+  auto position = [&](int at) { return POS && at >= 0 ? p.pos_pool[at] : 0; };
   auto judge = [&](int at, int pos, uint32_t* f) -> int {                          // the place, -1 if the row is not seen
     *f = 0;
     return POS && at >= 0 && !ca_seen<POS>(p, rows, pos, f) ? -1 : at;
@@ -814,8 +814,8 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     heads = min(GT, p.group - g0);
     q0 = static_cast<const T*>(p.q) + seg.b * p.q_sb + hq * p.q_sh;
     rows.table = p.table + (static_cast<int64_t>(seg.b) * p.num_kv_heads + h) * p.max_pages;
-    rows.rows = min(min(max(__ldg(p.lens + seg.b), 0), most), seg.tile1 * kCaTile);
-    rows.q_pos = POS ? __ldg(p.q_pos + seg.b) : 0;
+    rows.rows = min(min(max(p.lens[seg.b], 0), most), seg.tile1 * kCaTile);
+    rows.q_pos = POS ? p.q_pos[seg.b] : 0;
     first = seg.tile0 * kCaTile + warp * W::TR;
     int mine[kCaStages];
     int pos[kCaStages];
@@ -836,7 +836,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     if constexpr (sizeof(T) == 4) {
       float* q_shared = reinterpret_cast<float*>(ca_smem + WARPS * W::kRing) + q_buffer * (GT * (D + 4));
       for (int i = tid; i < GT * D; i += THREADS) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
-      if (POS == 2 && tid < GT) q_shared[GT * D + tid] = tid < heads ? __ldg(p.slopes + hq + tid) * 1.4426950408889634f : 0.f;
+      if (POS == 2 && tid < GT) q_shared[GT * D + tid] = tid < heads ? p.slopes[hq + tid] * 1.4426950408889634f : 0.f;
       sums.start(p, q_shared, heads, hq);
     } else {
       uint8_t* q_shared = ca_smem + WARPS * W::kRing + q_buffer * (GT * Sums::kQ);

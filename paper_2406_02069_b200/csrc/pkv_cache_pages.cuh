@@ -74,7 +74,7 @@ struct PgChild {
 };
 __device__ __forceinline__ int pg_parent(const PagesParams& p, int c) {
   if (!p.parents) return c;
-  const int par = __ldg(p.parents + c);
+  const int par = p.parents[c];
   return par < 0 || par >= p.from_batch ? -1 : par;
 }
 __device__ __forceinline__ PgChild pg_child(const PagesParams& p, int l, int c, int parent, bool first) {
@@ -85,7 +85,7 @@ __device__ __forceinline__ PgChild pg_child(const PagesParams& p, int l, int c, 
   x.full = x.rows / p.page_size;
   x.part = x.rows - x.full * p.page_size;
   x.keeps = x.full + (x.part > 0 && first ? 1 : 0);
-  const int add = p.add ? max(__ldg(p.add + l * p.add_stride + c), 0) : 0;
+  const int add = p.add ? max(p.add[l * p.add_stride + c], 0) : 0;
   x.rows_new = static_cast<int64_t>(x.rows) + add;
   x.pages = static_cast<int>(min(static_cast<int64_t>(INT32_MAX), (x.rows_new + p.page_size - 1) / p.page_size));
   return x;
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
       if (threadIdx.x == 0) s_first = 1;
       __syncthreads();
       for (int i = threadIdx.x; i < c; i += kPgCarryThreads)
-        if (__ldg(p.parents + i) == parent) s_first = 0;
+        if (p.parents[i] == parent) s_first = 0;
       __syncthreads();
       first = s_first != 0;
     }
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
   if (threadIdx.x == 0) s_first = 1;
   __syncthreads();
   for (int i = threadIdx.x; i < p.to_batch; i += kPgCarryThreads)
-    if (__ldg(p.parents + i) == b) s_first = 0;
+    if (p.parents[i] == b) s_first = 0;
   __syncthreads();
   if (!s_first) return;
   const int rows = pg_clamped(p.from.lens[static_cast<int64_t>(l) * p.from_batch + b], p);
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
     __syncthreads();
     for (int c = tid; c < p.to_batch; c += kPgThreads) {
       const int parent = pg_parent(p, c);
-      if (parent < 0 && __ldg(p.parents + c) != -1) bad |= 1;
+      if (parent < 0 && p.parents[c] != -1) bad |= 1;
       if (parent >= 0) atomicMin(&s_child[parent], c);
       s_parent[c] = parent;
     }
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_copy_kernel(const __gri
   if (threadIdx.x == 0) s_first = 1;
   __syncthreads();
   for (int i = threadIdx.x; i < c; i += kPgCarryThreads)
-    if (__ldg(p.parents + i) == parent) s_first = 0;
+    if (p.parents[i] == parent) s_first = 0;
   __syncthreads();
   const PgChild x = pg_child(p, l, c, parent, s_first != 0);
   if (x.first || !x.part) return;

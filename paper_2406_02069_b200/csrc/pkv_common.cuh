@@ -43,7 +43,9 @@ enum : uint32_t {
 // the kernel before it in the stream is still draining.  A kernel first lets its own successor be
 // scheduled (pdl_trigger), does whatever set-up touches no global memory, and then waits for the
 // preceding kernel to have completed and flushed its writes (pdl_wait) before it reads or writes
-// global memory.  Without a preceding kernel both are no-ops.
+// global memory.  Without a preceding kernel both are no-ops.  What kernels ahead may write (page tables, lengths,
+// positions) is read by plain loads: __ldg promises that memory stays as it is for as long as the kernel lives, and
+// that begins before the wait.
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -23,7 +23,7 @@ struct PageTable {
 
 // Row (in units of rows) of the pool that holds row r of head h of sequence b, or -1 for a bad table entry.
 __device__ __forceinline__ int64_t paged_row(const PageTable& t, int b, int h, int r) {
-  const int page = __ldg(t.table + t.tab_off[b] + static_cast<int64_t>(h) * t.pages[b] + r / t.page_size);
+  const int page = t.table[t.tab_off[b] + static_cast<int64_t>(h) * t.pages[b] + r / t.page_size];
   if (page < 0 || page >= t.num_pages) return -1;
   return static_cast<int64_t>(page) * t.page_size + r % t.page_size;
 }

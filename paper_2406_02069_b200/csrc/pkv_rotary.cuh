@@ -126,14 +126,14 @@ __global__ void __launch_bounds__(kRotThreads, kRotPerSm<VEC, APPEND>) rotary_ke
   int page_at = 0, slot_in_page = 0;
   bool inside = true;
   if (APPEND) {
-    const int count = p.counts ? min(max(__ldg(p.counts + b), 0), p.tokens) : p.tokens;
+    const int count = p.counts ? min(max(p.counts[b], 0), p.tokens) : p.tokens;
     if (t >= count) return;
-    const int64_t row = static_cast<int64_t>(__ldg(p.lens + b)) - count + t;
+    const int64_t row = static_cast<int64_t>(p.lens[b]) - count + t;
     inside = row >= 0 && row < static_cast<int64_t>(p.max_pages) * p.page_size;
     page_at = inside ? static_cast<int>(row / p.page_size) : 0;
     slot_in_page = inside ? static_cast<int>(row - static_cast<int64_t>(page_at) * p.page_size) : 0;
   }
-  const int pos = p.positions ? __ldg(p.positions + b * p.positions_stride + t) : 0;
+  const int pos = p.positions ? p.positions[b * p.positions_stride + t] : 0;
   const bool rotated = u < p.rot_units;
   // elements at which the unit's two pieces start
   const int r = 2 * p.half;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kRotThreads, kRotPerSm<VEC, APPEND>) rotary_ke
       a[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC : e0));
       c[i] = *reinterpret_cast<const Piece*>(from + (is_v ? u * 2 * VEC + VEC : e1));
       if (APPEND && !is_query(h))
-        page[i] = inside ? __ldg(p.table + (static_cast<int64_t>(b) * p.heads_kv + number(h)) * p.max_pages + page_at) : -1;
+        page[i] = inside ? p.table[(static_cast<int64_t>(b) * p.heads_kv + number(h)) * p.max_pages + page_at] : -1;
     }
   };
   const int first = blockIdx.y * p.head_lanes + hl;

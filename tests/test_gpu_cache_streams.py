@@ -189,3 +189,45 @@ def test_inactive_sequences_of_a_batch_are_left_alone():
     for h in range(2):                                               # a sequence that took nothing still attends to what it has
         w, _, size = attend(q[2, 2 * h:2 * h + 2, 0].cpu(), x.k[2][h], x.v[2][h])
         assert torch.all((out[2, 2 * h:2 * h + 2].cpu().double() - w).abs() <= 1e-4 * size + 1e-7)
+
+
+@pytest.mark.parametrize("page", [1, 4])
+def test_a_long_run_of_steps_with_nothing_waited_for(page):
+    """Reserve, append and attend sixty times in a row without looking: every step sees the lengths, pages and rows of the ones
+    ahead of it, although its kernels are on the device before those have finished."""
+    heads, group, d, steps, layers = 2, 4, 64, 60, 2
+    x = Pool(pkv.make_config(num_layers=layers, num_q_heads=heads * group, num_kv_heads=heads, head_dim=d, window=1, pool_kernel=1, dtype="bf16", avg_budget=1),
+             [[3, 0, 7]] * layers, page, 4 * (steps + 10) * 3 * heads * layers // page, steps // page + 12)
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(steps, layers, 3, h, 1, d, generator=g).to(torch.bfloat16) for h in (heads * group, heads, heads))
+    dq, dk, dv = q.to(DEV), k.to(DEV), v.to(DEV)
+    r = random.Random(page)
+    adds = [[1, r.choice([0, 1]), 1] for _ in range(steps)]
+    dadd = add_tensor(adds)
+    granted = torch.zeros(steps, layers, 3, dtype=torch.int32, device=DEV)
+    out = torch.zeros(steps, layers, 3, heads * group, d, device=DEV)
+    positions = torch.zeros(3, 1, dtype=torch.int32, device=DEV)
+    rows = [[[[p[x.lists.row(l, b, h, i) // page, x.lists.row(l, b, h, i) % page] for i in range(x.lists.lens[l][b])] for p in x.pools[:2]]
+             for b in range(3) for h in range(heads)] for l in range(layers)]
+    torch.cuda.synchronize()
+    for s in range(steps):
+        pkv.cache_reserve(x.cfg, x.cache, dadd[s], x.ws, granted=granted[s])
+        for l in range(layers):
+            pkv.append_cache(x.cfg, x.cache, l, positions, dk[s, l], dv[s, l], x.ws, counts=granted[s, l])
+            pkv.decode_attention_cache(x.cfg, x.cache, l, dq[s, l], out[s, l], x.ws)
+    pkv.check_status(x.ws)
+    got = out.cpu()
+    for s in range(steps):
+        for l in range(layers):
+            for b in range(3):
+                for h in range(heads):
+                    ks, vs = rows[l][b * heads + h]
+                    if adds[s][b]:
+                        ks.append(k[s, l, b, h, 0])
+                        vs.append(v[s, l, b, h, 0])
+                    hq = slice(h * group, (h + 1) * group)
+                    if not ks:
+                        assert torch.all(got[s, l, b, hq] == 0)
+                        continue
+                    want, _, size = attend(q[s, l, b, hq, 0], torch.stack(ks), torch.stack(vs))
+                    assert torch.all((got[s, l, b, hq].double() - want).abs() <= 1e-4 * size + 1e-7), (s, l, b, h)
