@@ -22,8 +22,13 @@ int elem_bytes(const pkv_config* c) { return c->dtype == PKV_DTYPE_FP32 ? 4 : 2;
 
 bool pointer_ok(const void* p, size_t align) { return p && reinterpret_cast<uintptr_t>(p) % align == 0; }
 
-// Query heads that a CTA of the attention takes.
-int heads_per_cta(const pkv_config* c) { return c->num_q_heads / c->num_kv_heads <= 4 ? 4 : 8; }
+// Query heads that a CTA of the attention takes.  16-bit rows: four cost what one does (they are rows of one product); fp32: each has
+// its own instructions (three sequences of up to 1231 rows, 32 heads of their own: 35 us four at a time, 28 one at a time).
+int heads_per_cta(const pkv_config* c) {
+  const int group = c->num_q_heads / c->num_kv_heads;
+  if (group >= 5) return 8;
+  return c->dtype == PKV_DTYPE_FP32 && group < 3 ? group : 4;
+}
 int head_blocks(const pkv_config* c) {
   const int group = c->num_q_heads / c->num_kv_heads, gt = heads_per_cta(c);
   return (group + gt - 1) / gt;
@@ -182,14 +187,19 @@ int launch_cache_attend(CacheAttendParams& p, int64_t max_rows, cudaStream_t st)
   return check_launch();
 }
 
+template <typename T, int D, int GT>
+int dispatch_positions(CacheAttendParams& p, int64_t max_rows, cudaStream_t st) {
+  if (!p.q_pos) return launch_cache_attend<T, D, GT, 0>(p, max_rows, st);
+  return p.slopes ? launch_cache_attend<T, D, GT, 2>(p, max_rows, st) : launch_cache_attend<T, D, GT, 1>(p, max_rows, st);
+}
+
 template <typename T, int D>
 int dispatch_cache_attend(CacheAttendParams& p, int gt, int64_t max_rows, cudaStream_t st) {
-  const int pos = !p.q_pos ? 0 : (p.slopes ? 2 : 1);
-  if (gt == 4)
-    return pos == 0 ? launch_cache_attend<T, D, 4, 0>(p, max_rows, st)
-                    : (pos == 1 ? launch_cache_attend<T, D, 4, 1>(p, max_rows, st) : launch_cache_attend<T, D, 4, 2>(p, max_rows, st));
-  return pos == 0 ? launch_cache_attend<T, D, 8, 0>(p, max_rows, st)
-                  : (pos == 1 ? launch_cache_attend<T, D, 8, 1>(p, max_rows, st) : launch_cache_attend<T, D, 8, 2>(p, max_rows, st));
+  if constexpr (sizeof(T) == 4) {
+    if (gt == 1) return dispatch_positions<T, D, 1>(p, max_rows, st);
+    if (gt == 2) return dispatch_positions<T, D, 2>(p, max_rows, st);
+  }
+  return gt == 4 ? dispatch_positions<T, D, 4>(p, max_rows, st) : dispatch_positions<T, D, 8>(p, max_rows, st);
 }
 
 // ---------------------------------------------------------------- pages

@@ -12,12 +12,12 @@
 //   * A CTA that has all tiles of a head writes its output; otherwise it leaves (exponent, sum, weighted sum) in the workspace, and
 //     the last CTA of the head to arrive joins them in the order of the rows (many of them in groups first), so that equal calls
 //     give equal bits.
-//   * A warp takes tiles of 16 rows, kStages of them in shared memory or on their way by asynchronous copies.  A row that is
+//   * A warp takes tiles of 16 rows (fp32: 8), kCaStages of them in shared memory or on their way by asynchronous copies.  A row that is
 //     not seen is filled with zeros instead of read; a tile without a seen row costs its positions only.
 //   * 16-bit rows go through mma.sync, fp32 accumulation, the query heads as M: GT = 4 heads with the high, middle and low
 //     16-bit parts of their softmax weights in rows 0-3, 4-7 and 8-11, GT = 8 with high and middle parts in one product and
 //     the low ones in a second.  The parts carry 24 bits, so the weights stay fp32 in effect.
-//   * fp32 rows: a lane has half a row's dot products, then a few channels of all rows.
+//   * fp32 rows: a lane has a quarter of a row's dot products, then four channels of all rows; GT = 1, 2, 4 or 8.
 #pragma once
 
 #include "pkv_common.cuh"
