@@ -46,6 +46,7 @@ int cache_check(const pkv_config* c, const pkv_cache* x) {
     return PKV_ERR_UNSUPPORTED;
   if ((rows + kCaTile - 1) / kCaTile * x->batch > INT32_MAX) return PKV_ERR_UNSUPPORTED;      // tiles of a head
   if (static_cast<int64_t>(x->batch) * c->num_kv_heads * head_blocks(c) > kMaxUnits) return PKV_ERR_UNSUPPORTED;
+  static_assert(int64_t{PKV_MAX_CACHE_BATCH} * 65535 < INT32_MAX, "sequences of all layers are counted in 32 bits");
   return PKV_OK;
 }
 
@@ -55,7 +56,6 @@ struct CacheWorkspace {
   int32_t* group_counters;
   int32_t* state;
   float* partials;
-  int32_t* unit_off;
   int32_t* list;
   int32_t* second;
   int32_t* place;
@@ -78,7 +78,6 @@ CacheWorkspace carve_cache(const pkv_config* c, const pkv_cache* x, void* base) 
   w.counters = static_cast<int32_t*>(take(kMaxUnits * 4));
   w.group_counters = static_cast<int32_t*>(take(size_t{2} * kCaMaxGrid * 4));
   w.partials = static_cast<float*>(take(size_t{2} * kCaMaxGrid * kCaPartial * sizeof(float)));
-  w.unit_off = static_cast<int32_t*>(take(units * 4));
   w.list = static_cast<int32_t*>(take(pages * 4));
   w.second = static_cast<int32_t*>(take(pages * 4));
   w.place = static_cast<int32_t*>(take(pages * 4));
@@ -262,7 +261,6 @@ int pages_setup(const pkv_config* c, const pkv_cache* from, const pkv_cache* to,
   p->list = w.list;
   p->second = w.second;
   p->place = w.place;
-  p->unit_off = w.unit_off;
   p->staged = w.staged;
   return PKV_OK;
 }

@@ -54,14 +54,13 @@ struct PagesParams {
   int32_t* list;                           // [num_pages] dealt pages; compaction: free pages to move into
   int32_t* second;                         // [num_pages] compaction: pages that move
   int32_t* place;                          // [num_pages] compaction: new place of every page from the border on
-  int32_t* unit_off;                       // [layers * to_batch] requests ahead of a sequence's
 };
 
 __device__ __forceinline__ int32_t pg_clamped(int32_t rows, const PagesParams& p) {
   const int64_t most = static_cast<int64_t>(p.max_pages) * p.page_size;
   return static_cast<int32_t>(min(static_cast<int64_t>(max(rows, 0)), most));
 }
-__device__ __forceinline__ int pg_pages(const PagesParams& p, int64_t rows) { return static_cast<int>((rows + p.page_size - 1) / p.page_size); }
+__device__ __forceinline__ int pg_pages(const PagesParams& p, int rows) { return rows / p.page_size + (rows % p.page_size ? 1 : 0); }
 
 // What sequence c of `to` becomes in a layer.
 struct PgChild {
@@ -69,7 +68,7 @@ struct PgChild {
   bool first;                              // its parent's first child
   int32_t rows, full, part;                // of the parent: rows, full pages, rows of the last page if it is not full
   int32_t keeps;                           // pages whose entries it takes over
-  int64_t rows_new;
+  uint32_t rows_new;                       // (below 2^30 + 2^31)
   int pages;
 };
 __device__ __forceinline__ int pg_parent(const PagesParams& p, int c) {
@@ -86,8 +85,9 @@ __device__ __forceinline__ PgChild pg_child(const PagesParams& p, int l, int c, 
   x.part = x.rows - x.full * p.page_size;
   x.keeps = x.full + (x.part > 0 && first ? 1 : 0);
   const int add = p.add ? max(p.add[l * p.add_stride + c], 0) : 0;
-  x.rows_new = static_cast<int64_t>(x.rows) + add;
-  x.pages = static_cast<int>(min(static_cast<int64_t>(INT32_MAX), (x.rows_new + p.page_size - 1) / p.page_size));
+  x.rows_new = static_cast<uint32_t>(x.rows) + static_cast<uint32_t>(add);
+  const uint32_t pages = x.rows_new / static_cast<uint32_t>(p.page_size);
+  x.pages = static_cast<int>(min(pages + (pages * p.page_size < x.rows_new ? 1u : 0u), static_cast<uint32_t>(INT32_MAX)));
   return x;
 }
 
@@ -139,12 +139,14 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
     if (parent < 0) return;
     const int64_t src = (static_cast<int64_t>(l) * p.from_batch + parent) * p.num_kv_heads * p.max_pages;
     const int64_t dst = (static_cast<int64_t>(l) * p.to_batch + c) * p.num_kv_heads * p.max_pages;
-    const int64_t keeps = x.keeps, all = keeps * p.num_kv_heads;
-    for (int64_t i = threadIdx.x; i < all; i += kPgCarryThreads) {
-      const int64_t h = i / keeps, j = i - h * keeps;
-      const int entry = p.from.tables[src + h * p.max_pages + j];
-      p.to.tables[dst + h * p.max_pages + j] = entry;
-      if (!x.first && entry >= 0 && entry < p.num_pages) atomicAdd(p.to.refs + entry, 1);
+    for (int h = threadIdx.x >> 5; h < p.num_kv_heads; h += kPgCarryThreads / 32) {        // a warp per head
+      const int32_t* from = p.from.tables + src + static_cast<int64_t>(h) * p.max_pages;
+      int32_t* to = p.to.tables + dst + static_cast<int64_t>(h) * p.max_pages;
+      for (int j = threadIdx.x & 31; j < x.keeps; j += 32) {
+        const int entry = from[j];
+        to[j] = entry;
+        if (!x.first && entry >= 0 && entry < p.num_pages) atomicAdd(p.to.refs + entry, 1);
+      }
     }
     return;
   }
@@ -157,20 +159,20 @@ __global__ void __launch_bounds__(kPgCarryThreads) pages_carry_kernel(const __gr
   __syncthreads();
   if (!s_first) return;
   const int rows = pg_clamped(p.from.lens[static_cast<int64_t>(l) * p.from_batch + b], p);
-  const int64_t pages = pg_pages(p, rows), all = pages * p.num_kv_heads;
+  const int pages = pg_pages(p, rows);
   const int64_t src = (static_cast<int64_t>(l) * p.from_batch + b) * p.num_kv_heads * p.max_pages;
-  for (int64_t i = threadIdx.x; i < all; i += kPgCarryThreads) {
-    const int64_t h = i / pages, j = i - h * pages;
-    const int entry = p.from.tables[src + h * p.max_pages + j];
-    if (entry >= 0 && entry < p.num_pages) atomicSub(p.to.refs + entry, 1);
-  }
+  for (int h = threadIdx.x >> 5; h < p.num_kv_heads; h += kPgCarryThreads / 32)
+    for (int j = threadIdx.x & 31; j < pages; j += 32) {
+      const int entry = p.from.tables[src + static_cast<int64_t>(h) * p.max_pages + j];
+      if (entry >= 0 && entry < p.num_pages) atomicSub(p.to.refs + entry, 1);
+    }
 }
 
 // ------------------------------------------------------------------ 2. sums and ranks over a cluster
 struct PgShared {
   long long warp[32];
-  int32_t block[2];                        // this CTA's sums, read by the others; each is used once
-  int32_t flag;
+  int32_t need[kPgCluster], free[kPgCluster], flag[kPgCluster];  // of every CTA, written by it ahead of the cluster's barrier
+  int32_t bad;
 };
 
 // Exclusive running sum over the CTA's threads; *total: the CTA's sum.  Everybody takes part.
@@ -197,15 +199,19 @@ __device__ __forceinline__ I pg_scan(PgShared& s, I x, I* total) {
   return run - x + (warp ? ahead : I(0));
 }
 
-// What the CTAs ahead have of one of the sums, and all of them; behind a barrier of the cluster.
-__device__ __forceinline__ void pg_cluster(PgShared& s, int which, int* ahead, int* total) {
+// Every CTA gets this one's number; there behind a barrier of the cluster.  (Read from the others behind it: 1.6 us for three.)
+__device__ __forceinline__ void pg_tell(int32_t (&of)[kPgCluster], int32_t x) {
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
+  if (threadIdx.x < kPgCluster) *cluster.map_shared_rank(&of[cluster.block_rank()], threadIdx.x) = x;
+}
+
+// What the CTAs ahead have of a number, and all of them.
+__device__ __forceinline__ void pg_cluster(const int32_t (&of)[kPgCluster], int rank, int* ahead, int* total) {
   *ahead = *total = 0;
-  const int rank = static_cast<int>(cluster.block_rank());
 #pragma unroll
   for (int c = 0; c < kPgCluster; ++c) {
-    const int x = *cluster.map_shared_rank(&s.block[which], c);
+    const int x = of[c];
     if (c < rank) *ahead += x;
     *total += x;
   }
@@ -275,8 +281,14 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   __shared__ int32_t s_child[PKV_MAX_CACHE_BATCH];               // a parent's first child
   pdl_trigger();
   const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // this CTA's shared memory may be written
   pdl_wait();
-  if (tid == 0) s.flag = 0;
+  if (tid == 0) s.bad = 0;
+  const bool aligned = reinterpret_cast<uintptr_t>(p.to.refs) % 16 == 0;
+  int64_t lo, hi;
+  pg_share(p.num_pages, rank, &lo, &hi);
+  PgFree free;
+  const int my_free = free.count(p.to.refs, aligned, lo, hi);
   int bad = 0;                             // bit 0: a parent outside the batch, bit 1: a sequence too long for its table
   if (p.parents) {
     for (int b = tid; b < p.from_batch; b += kPgThreads) s_child[b] = INT32_MAX;
@@ -292,46 +304,42 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
       if (s_parent[c] >= 0 && s_child[s_parent[c]] != c) s_parent[c] |= 1 << 30;
   }
   __syncthreads();
-  const int64_t units = static_cast<int64_t>(p.layers) * p.to_batch;
-  const int worker = rank * kPgThreads + tid;
-  constexpr int kWorkers = kPgCluster * kPgThreads;
-  auto child = [&](int64_t unit) {
-    const int l = static_cast<int>(unit / p.to_batch), c = static_cast<int>(unit - static_cast<int64_t>(l) * p.to_batch);
+  const int units = p.layers * p.to_batch;
+  auto child = [&](int unit) {
+    const int l = unit / p.to_batch, c = unit - l * p.to_batch;
     const int x = p.parents ? s_parent[c] : c;
     return pg_child(p, l, c, x < 0 ? -1 : x & ~(1 << 30), x >= 0 && !(x >> 30));
   };
   // requests of every unit; each thread has consecutive ones
-  const int64_t per = (units + kWorkers - 1) / kWorkers, u0 = min(units, per * worker), u1 = min(units, u0 + per);
+  constexpr int kWorkers = kPgCluster * kPgThreads;
+  const int per = (units + kWorkers - 1) / kWorkers, u0 = min(units, per * (rank * kPgThreads + tid)), u1 = min(units, u0 + per);
   int64_t mine = 0;
-  for (int64_t u = u0; u < u1; ++u) {
+  for (int u = u0; u < u1; ++u) {
     const PgChild x = child(u);
     if (x.pages > p.max_pages) bad |= 2;
     else mine += static_cast<int64_t>(x.pages - x.keeps) * p.num_kv_heads;
   }
-  // more requests than pages cannot be met; sums stay within 32 bits that way
+  // more requests than pages cannot be met; sums stay within bounds that way
   if (mine > p.num_pages) { bad |= 2; mine = 0; }
-  if (bad) atomicOr(&s.flag, bad);
-  int64_t lo, hi;
-  pg_share(p.num_pages, rank, &lo, &hi);
-  const bool aligned = reinterpret_cast<uintptr_t>(p.to.refs) % 16 == 0;
-  PgFree free;
-  const int my_free = free.count(p.to.refs, aligned, lo, hi);
-  long long cta_need;
-  int cta_free;
-  const long long run_need = pg_scan<long long>(s, mine, &cta_need);
-  const int run_free = __shfl_sync(0xffffffffu, pg_scan<int>(s, (tid & 31) == 0 ? my_free : 0, &cta_free), 0);
-  if (tid == 0) {
-    if (cta_need > p.num_pages) s.flag |= 2;
-    s.block[0] = cta_need > p.num_pages ? 0 : static_cast<int>(cta_need);
-    s.block[1] = cta_free;
-  }
+  if (bad) atomicOr(&s.bad, bad);
+  // one scan for both: requests (at most 2^27 of 1024 threads) in 38 bits, free pages (at most 2^24 of a CTA) above
+  constexpr int kBits = 38;
+  const long long ours = mine + (static_cast<long long>((tid & 31) == 0 ? my_free : 0) << kBits);
+  long long cta;
+  const long long run = pg_scan<long long>(s, ours, &cta);
+  const long long run_need = run & ((1ll << kBits) - 1), cta_need = cta & ((1ll << kBits) - 1);
+  const int run_free = __shfl_sync(0xffffffffu, static_cast<int>(run >> kBits), 0);
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");    // and everybody else's
+  pg_tell(s.need, cta_need > p.num_pages ? 0 : static_cast<int>(cta_need));
+  pg_tell(s.free, static_cast<int>(cta >> kBits));
+  pg_tell(s.flag, s.bad | (cta_need > p.num_pages ? 2 : 0));
   cluster.sync();
   int ahead, need, place, free_all, flags = 0;
-  pg_cluster(s, 0, &ahead, &need);
-  pg_cluster(s, 1, &place, &free_all);
+  pg_cluster(s.need, rank, &ahead, &need);
+  pg_cluster(s.free, rank, &place, &free_all);
   place += run_free;                       // the rank of this warp's first free page
 #pragma unroll
-  for (int c = 0; c < kPgCluster; ++c) flags |= *cluster.map_shared_rank(&s.flag, c);
+  for (int c = 0; c < kPgCluster; ++c) flags |= s.flag[c];
   const bool met = flags == 0 && need <= free_all;               // (sums of eight shares of at most 2^27)
   if (rank == 0 && tid == 0) {
     p.state[0] = met ? 1 : 0;
@@ -339,8 +347,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
   }
   if (!met) {                              // the same in the whole cluster
     if (p.granted)
-      for (int64_t u = u0; u < u1; ++u) p.granted[u] = 0;
-    cluster.sync();                        // nobody leaves while its sums are read
+      for (int u = u0; u < u1; ++u) p.granted[u] = 0;
     return;
   }
   int t = 0;
@@ -360,44 +367,51 @@ __global__ void __launch_bounds__(kPgThreads) pages_deal_kernel(const __grid_con
         ++r;
       }
   }
+  cluster.sync();                          // the list is there (and so are everybody's reads of parents' lens)
+  // Table entries of this thread's units, their pages one after another in the list, head by head.  Many of them: by the whole warp.
+  // (A warp per head of a unit, one after another: 79 us for 64 sequences x 32 layers x 8 heads, 19 with a lane per head, 15 this way, all with a cold L2.)
+  constexpr int kAlone = 32;
   int64_t off = ahead + run_need;
-  for (int64_t u = u0; u < u1; ++u) {
-    const PgChild x = child(u);
-    p.unit_off[u] = static_cast<int32_t>(off);
-    off += static_cast<int64_t>(x.pages - x.keeps) * p.num_kv_heads;
-  }
-  cluster.sync();                          // list and offsets are there (and so are everybody's reads of lens)
-  // table entries: a lane has a head of a unit; where that needs many pages, its warp writes them together
-  // (a warp per head throughout: 79 us for 64 sequences x 32 layers x 8 heads, 19 this way, both with a cold L2)
-  constexpr int kAlone = 4;
-  const int lane = tid & 31;
-  const int64_t heads = units * p.num_kv_heads;
-  for (int64_t i0 = worker - lane; i0 < heads; i0 += kWorkers) {
-    const int64_t i = i0 + lane;
-    const int32_t* pages = p.list;
+  for (int i = 0; i < per; ++i) {          // (uniform over the warp)
+    const int u = u0 + i;
+    const int32_t* pages = p.list + off;
     int32_t* table = p.to.tables;
-    int fresh = 0;
-    if (i < heads) {
-      const int64_t u = i / p.num_kv_heads;
+    int fresh = 0, all = 0;
+    if (u < u1) {
       const PgChild x = child(u);
       fresh = x.pages - x.keeps;
-      if (fresh) pages += __ldcg(p.unit_off + u) + (i - u * p.num_kv_heads) * fresh;
-      table += i * p.max_pages + x.keeps;
+      all = fresh * p.num_kv_heads;        // (at most num_pages)
+      off += all;
+      table += static_cast<int64_t>(u) * p.num_kv_heads * p.max_pages + x.keeps;
+      p.to.lens[u] = static_cast<int32_t>(x.rows_new);
+      if (p.granted) p.granted[u] = static_cast<int32_t>(x.rows_new) - x.rows;
     }
-    if (fresh <= kAlone)
-      for (int j = 0; j < fresh; ++j) table[j] = __ldcg(pages + j);
-    for (unsigned many = __ballot_sync(0xffffffffu, fresh > kAlone); many; many &= many - 1) {
-      const int l = __ffs(many) - 1, n = __shfl_sync(0xffffffffu, fresh, l);
+    if (all <= kAlone) {
+      constexpr int kAhead = 8;            // entries on their way at a time
+      for (int e = 0, h = 0, j = 0; e < all; e += kAhead) {
+        int32_t page[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) page[i] = __ldcg(pages + min(e + i, all - 1));
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (e + i < all) {
+            table[static_cast<int64_t>(h) * p.max_pages + j] = page[i];
+            if (++j == fresh) {
+              j = 0;
+              ++h;
+            }
+          }
+      }
+    }
+    for (unsigned many = __ballot_sync(0xffffffffu, all > kAlone); many; many &= many - 1) {
+      const int l = __ffs(many) - 1, n = __shfl_sync(0xffffffffu, fresh, l), sum = __shfl_sync(0xffffffffu, all, l);
       const int32_t* from = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(pages), l));
       int32_t* to = reinterpret_cast<int32_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(table), l));
-      for (int j = lane; j < n; j += 32) to[j] = __ldcg(from + j);
+      for (int e = tid & 31; e < sum; e += 32) {
+        const int h = e / n;
+        to[static_cast<int64_t>(h) * p.max_pages + (e - h * n)] = __ldcg(from + e);
+      }
     }
-  }
-  if (p.in_place) cluster.sync();          // lens of `from` are those of `to`: they change behind everybody's last look
-  for (int64_t u = u0; u < u1; ++u) {
-    const PgChild x = child(u);
-    p.to.lens[u] = static_cast<int32_t>(x.rows_new);
-    if (p.granted) p.granted[u] = static_cast<int32_t>(x.rows_new - x.rows);
   }
 }
 
@@ -472,6 +486,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_con
   __shared__ PgShared s;
   pdl_trigger();
   const int rank = static_cast<int>(cluster.block_rank()), tid = threadIdx.x;
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");  // this CTA's shared memory may be written
   pdl_wait();
   const int32_t* refs = p.from.refs;
   const bool aligned = reinterpret_cast<uintptr_t>(refs) % 16 == 0;
@@ -481,9 +496,10 @@ __global__ void __launch_bounds__(kPgThreads) pages_pair_kernel(const __grid_con
   const int mine = free.count(refs, aligned, lo, hi);
   int cta, ahead, all;
   const int run = __shfl_sync(0xffffffffu, pg_scan<int>(s, (tid & 31) == 0 ? mine : 0, &cta), 0);
-  if (tid == 0) s.block[0] = cta;
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");    // and everybody else's
+  pg_tell(s.free, cta);
   cluster.sync();
-  pg_cluster(s, 0, &ahead, &all);
+  pg_cluster(s.free, rank, &ahead, &all);
   ahead += run;                            // free pages ahead of this warp's
   const int used = p.num_pages - all;
   // The warp whose share the border lies in (the last one with pages, if that is the pool's end) counts the free pages below it.
@@ -577,13 +593,13 @@ __global__ void __launch_bounds__(kPgCopyThreads) pages_move_kernel(const __grid
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int rows = p.from.lens[unit];
     const int pages = pg_pages(p, pg_clamped(rows, p));
-    const int64_t at = unit * p.num_kv_heads * p.max_pages, all = static_cast<int64_t>(pages) * p.num_kv_heads;
-    for (int64_t i = threadIdx.x; i < all; i += kPgCopyThreads) {
-      const int64_t h = i / pages, e = at + h * p.max_pages + (i - h * pages);
-      const int entry = p.from.tables[e];
-      const int place = entry >= used && entry < p.num_pages ? p.place[entry] : entry;
-      if (!p.in_place || place != entry) p.to.tables[e] = place;
-    }
+    for (int h = threadIdx.x >> 5; h < p.num_kv_heads; h += kPgCopyThreads / 32)
+      for (int j = threadIdx.x & 31; j < pages; j += 32) {
+        const int64_t e = (unit * p.num_kv_heads + h) * p.max_pages + j;
+        const int entry = p.from.tables[e];
+        const int place = entry >= used && entry < p.num_pages ? p.place[entry] : entry;
+        if (!p.in_place || place != entry) p.to.tables[e] = place;
+      }
     if (!p.in_place && threadIdx.x == 0) p.to.lens[unit] = rows;
   }
   // A free page below the border has its new tenant's count, a page from the border on none.
