@@ -586,8 +586,9 @@ typedef struct pkv_cache {
 size_t pyramidkv_cache_workspace_bytes(const pkv_config* cfg, const pkv_cache* cache);
 
 /*
- * Limits of the calls below (PKV_ERR_UNSUPPORTED beyond): 1024 sequences, 2^27 pages, 2^31 rows of a pool, 2^30 rows of a
- * sequence's table, 65536 blocks of four (more than four query heads to a KV head: eight) query heads in the batch.
+ * Limits of the calls below (PKV_ERR_UNSUPPORTED beyond): 65535 query heads, 65535 layers, 1024 sequences, 2^27 pages, 2^31
+ * rows of a pool, 2^30 rows of a sequence's table, 65536 blocks of query heads in the batch (blocks of four, of eight where
+ * more than four share a KV head; fp32 also of one and two).
  *
  * Rotary positions.  Element pairs (x, y) of a row at position p are turned by the angle p * frequency[i] and scaled:
  *     x' = magnitude * (x cos - y sin),   y' = magnitude * (y cos + x sin),    i = 0 .. rotary_dim / 2 - 1

@@ -41,7 +41,7 @@ int cache_check(const pkv_config* c, const pkv_cache* x) {
   if ((x->positions && !pointer_ok(x->positions, 4)) || (x->refs && !pointer_ok(x->refs, 4))) return PKV_ERR_INVALID_ARG;
   if (x->num_pages < 1 || x->page_size < 1 || x->layers < 1 || x->batch < 1 || x->max_pages < 1) return PKV_ERR_INVALID_ARG;
   const int64_t rows = static_cast<int64_t>(x->max_pages) * x->page_size;
-  if (x->batch > PKV_MAX_CACHE_BATCH || x->layers > 65535 || c->num_kv_heads > 65535 || x->num_pages > kMaxPages || rows > kMaxRows ||
+  if (x->batch > PKV_MAX_CACHE_BATCH || x->layers > 65535 || c->num_q_heads > 65535 || x->num_pages > kMaxPages || rows > kMaxRows ||
       static_cast<int64_t>(x->num_pages) * x->page_size > INT32_MAX)
     return PKV_ERR_UNSUPPORTED;
   if ((rows + kCaTile - 1) / kCaTile * x->batch > INT32_MAX) return PKV_ERR_UNSUPPORTED;      // tiles of a head
@@ -337,6 +337,7 @@ int pyramidkv_rotary(const pkv_config* cfg, const pkv_rotary* plan, const int32_
   if (!config_ok(cfg) || !plan || !positions || reinterpret_cast<uintptr_t>(positions) % 4) return PKV_ERR_INVALID_ARG;
   if (const int st = config_supported(cfg)) return st;
   if (!plan_ok(cfg, plan) || !tokens_ok(batch, tokens)) return PKV_ERR_INVALID_ARG;
+  if (cfg->num_q_heads > 65535) return PKV_ERR_UNSUPPORTED;
   const int d = cfg->head_dim, e = elem_bytes(cfg);
   if (!q.ptr != !q_out.ptr || !k.ptr != !k_out.ptr || (!q.ptr && !k.ptr)) return PKV_ERR_INVALID_ARG;
   RotaryParams p{};

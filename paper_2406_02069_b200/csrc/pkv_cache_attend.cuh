@@ -798,7 +798,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
   // Rows are looked up in two steps, a tile apart: a row's place, then its position.  Lane l has row l % TR.
   auto place = [&](int t0) { return ca_place<POS>(p, rows, t0 + lane % W::TR, lane < W::TR); };
   auto position = [&](int at) { return POS && at >= 0 ? p.pos_pool[at] : 0; };
-  auto judge = [&](int at, int pos, uint32_t* f) -> int {                          // the place, -1 if the row is not seen
+  auto check = [&](int at, int pos, uint32_t* f) -> int {                          // the place, -1 if the row is not seen
     *f = 0;
     return POS && at >= 0 && !ca_seen<POS>(p, rows, pos, f) ? -1 : at;
   };
@@ -827,7 +827,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     next_pos = position(next);
 #pragma unroll
     for (int s = 0; s < kCaStages; ++s) {
-      mine[s] = judge(mine[s], pos[s], &far[s]);
+      mine[s] = check(mine[s], pos[s], &far[s]);
       seen[s] = __ballot_sync(0xffffffffu, mine[s] >= 0) & kRowBits;
       if (s < kCaStages - 1) copy_in(s * kSlot, seen[s], mine[s]);
     }
@@ -868,7 +868,7 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
         seen[s] = seen[s + 1];
         far[s] = far[s + 1];
       }
-      const int mine = judge(next, next_pos, &far[kCaStages - 1]);
+      const int mine = check(next, next_pos, &far[kCaStages - 1]);
       seen[kCaStages - 1] = __ballot_sync(0xffffffffu, mine >= 0) & kRowBits;
       copy_in(slot, seen[kCaStages - 1], mine);
       next = second;

@@ -122,6 +122,8 @@ def test_configurations_are_checked_first():
     for bad, status in ((config(num_q_heads=7), INVALID), (config(head_dim=96), UNSUPPORTED), (config(window=0), INVALID)):
         assert append(cfg=bad) == status and attend(cfg=bad) == status
         assert rotary(cfg=bad, k=tensor(), k_out=tensor()) == status
+    wide = config(num_q_heads=65536, num_kv_heads=1)
+    assert append(cfg=wide) == UNSUPPORTED and attend(cfg=wide) == UNSUPPORTED and rotary(cfg=wide, k=tensor(), k_out=tensor()) == UNSUPPORTED
     many = config(num_q_heads=1024, num_kv_heads=256)
     assert attend(cfg=many, c=cache(batch=257)) == UNSUPPORTED              # more blocks of query heads than counters
 
