@@ -4,7 +4,9 @@
 //   s = q . k_r scale,   x = cap tanh(s / cap) - slope_g (p - p_r),   row seen if p_r <= p and (p - p_r < window or p_r < prefix)
 //
 // What bounds it: every seen row is read once, 2 d elements for 4 d operations per query head, so the floor is the bytes of
-// the cache over the memory bandwidth; a call with few rows is a chain of latencies (lengths, table, rows, join).
+// the cache over the memory bandwidth (64 sequences of 129 to 4096 rows, 32 / 8 heads, bf16: 93 us, 89 % of the rate of a copy;
+// 131072 rows of one: 98, 83 %); a call with few rows is a chain of latencies (64 rows: 5.4 us, of which lengths and plan 1.5,
+// table and queries 0.7, rows and products 1.0, merge and output 0.6; 512 rows in eight parts: 8.2).
 //   * The lengths are not known on the host, so the grid does not depend on them: as many CTAs as fit on the device at once,
 //     which deal the batch's tiles (64 rows of one KV head and block of query heads) out among themselves (CaPlan).  A long
 //     sequence is split over many CTAs, and a CTA takes many short ones in turn, the next one's rows on their way while
@@ -475,10 +477,25 @@ struct CaSums<float, D, GT, POS> {
 // Factor of sums that are relative to 2^m in sums relative to 2^largest.
 __device__ __forceinline__ float ca_factor(float m, float largest) { return m == -INFINITY ? 0.f : exp2f(m - largest); }
 
-// Writes a head's output: acc and z are relative to 2^m.  A sum of zero means that no row was seen.
-__device__ __forceinline__ void ca_write(const CacheAttendParams& p, int64_t head, int D, int channel, float m, float z, float acc) {
-  p.out[head * D + channel] = z == 0.f ? 0.f : acc / z;
+// Writes four channels of a head's output: acc and z are relative to 2^m.  A sum of zero means that no row was seen.
+__device__ __forceinline__ void ca_write(const CacheAttendParams& p, int64_t head, int D, int channel, float m, float z, float4 acc) {
+  float* to = p.out + head * D + channel;
+  const float4 v = z == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(acc.x / z, acc.y / z, acc.z / z, acc.w / z);
+  if (reinterpret_cast<uintptr_t>(p.out) % 16 == 0) {
+    *reinterpret_cast<float4*>(to) = v;
+  } else {                                 // (the output is as aligned as a float)
+    to[0] = v.x;
+    to[1] = v.y;
+    to[2] = v.z;
+    to[3] = v.w;
+  }
   if (channel == 0 && p.lse) p.lse[head] = z == 0.f ? -INFINITY : (m + log2f(z)) * 0.6931471805599453f;
+}
+__device__ __forceinline__ void ca_add(float4& a, const float4& x, float f) {
+  a.x = fmaf(x.x, f, a.x);
+  a.y = fmaf(x.y, f, a.y);
+  a.z = fmaf(x.z, f, a.z);
+  a.w = fmaf(x.w, f, a.w);
 }
 
 // A unit's partial results: where they lie, in the order of its rows.
@@ -539,24 +556,13 @@ __device__ __forceinline__ void ca_join(const CacheAttendParams& p, uint8_t* las
       if (i > 0 || o >= kCaThreads<T> * 4) fetch(i, o);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        if (i + j < count) {
-          const float f = factor(i + j)[g];
-          a.x = fmaf(x[j].x, f, a.x);
-          a.y = fmaf(x[j].y, f, a.y);
-          a.z = fmaf(x[j].z, f, a.z);
-          a.w = fmaf(x[j].w, f, a.w);
-        }
+        if (i + j < count) ca_add(a, x[j], factor(i + j)[g]);
       }
     }
     if (part) {
       __stcg(reinterpret_cast<float4*>(partial(0) + o), a);
     } else {
-      const float m = s_jm[g], z = s_jz[g];
-      const int channel = o - g * D;
-      ca_write(p, head0 + g, D, channel, m, z, a.x);
-      ca_write(p, head0 + g, D, channel + 1, m, z, a.y);
-      ca_write(p, head0 + g, D, channel + 2, m, z, a.z);
-      ca_write(p, head0 + g, D, channel + 3, m, z, a.w);
+      ca_write(p, head0 + g, D, o - g * D, s_jm[g], s_jz[g], a);
     }
   }
   if (part && threadIdx.x < heads) {
@@ -589,8 +595,9 @@ __device__ __forceinline__ bool ca_last(int32_t* counter, int of, int32_t* s_las
 // 14.6 us in equal ranges, where nearly every CTA has the end of one unit and the start of another.)
 constexpr int kCaStart = 2;
 constexpr int kCaSpare = 3;                // tiles that parts may have more than equal ranges would
-// A split has to save so many tiles in turn: handing sums over and joining them takes 2.8 us, a tile about 1 (128 rows of one
-// sequence, 8 KV heads: 8.8 us in two parts, 7.4 in one; 512 rows: 9.2 in eight, 10.0 in four, 11.5 in two).
+// A split has to save so many tiles in turn: handing sums over and joining them takes 2.8 us, a tile about 1 (one sequence, 8 KV
+// heads, while every call took 1.1 us longer than now: 128 rows 8.8 us in two parts, 7.4 in one; 512 rows 9.2 in eight, 10.0 in
+// four, 11.5 in two).
 constexpr int kCaSplit = 3;
 
 struct CaSegment {
@@ -661,6 +668,10 @@ __device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq,
   }
   int most = 0;                            // tiles of a part, 0: equal ranges
   if (static_cast<int64_t>(batch) * per_seq <= ctas && all < (1 << 30)) {
+    int longest = 0;
+    for (int s = lane; s < batch; s += 32) longest = max(longest, off[s + 1] - off[s]);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (longest <= kCaSplit) most = longest;                       // no split saves enough
     const unsigned units = batch * per_seq, tiles = static_cast<unsigned>(all);
     auto parts = [&](unsigned most) {
       unsigned sum = 0;
@@ -669,17 +680,13 @@ __device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq,
     };
     unsigned lo = (tiles + ctas - 1) / ctas, hi = units < ctas ? (tiles + ctas - units - 1) / (ctas - units) : off[batch];
     hi = max(lo, hi);                      // parts of hi tiles fit: there are fewer than tiles / hi + units of them
-    while (lo < hi) {
+    while (most == 0 && lo < hi) {
       const unsigned mid = (lo + hi) / 2;
       if (parts(mid) <= ctas) hi = mid;
       else lo = mid + 1;
     }
-    if (static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas) {
-      int longest = 0;
-      for (int s = lane; s < batch; s += 32) longest = max(longest, off[s + 1] - off[s]);
-      longest = __reduce_max_sync(0xffffffffu, longest);
+    if (most == 0 && static_cast<int64_t>(hi) * ctas <= all + static_cast<int64_t>(kCaSpare) * ctas)
       most = longest < static_cast<int>(hi) + kCaSplit ? longest : static_cast<int>(hi);
-    }
   }
   __syncwarp();
   if (most == 0) {
@@ -712,8 +719,9 @@ __device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq,
         const int unit = in_seq / x, k = in_seq - unit * x;
         seg[0].b = b;
         seg[0].unit = unit;
-        seg[0].tile0 = static_cast<int>(static_cast<int64_t>(tiles) * k / x);
-        seg[0].tile1 = static_cast<int>(static_cast<int64_t>(tiles) * (k + 1) / x);
+        const int each = tiles / x, longer = tiles - each * x;   // the first ones have a tile more
+        seg[0].tile0 = k * each + min(k, longer);
+        seg[0].tile1 = seg[0].tile0 + each + (k < longer ? 1 : 0);
         seg[0].whole = x == 1;
         seg[0].slot = 2 * cta;
         seg[0].first = seg[0].rest = 2 * (cta - k);
@@ -817,6 +825,12 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     rows.rows = min(min(max(p.lens[seg.b], 0), most), seg.tile1 * kCaTile);
     rows.q_pos = POS ? p.q_pos[seg.b] : 0;
     first = seg.tile0 * kCaTile + warp * W::TR;
+    // the queries: a 16-byte piece to a thread, on its way while the rows are looked up
+    constexpr int kPiece = 16 / static_cast<int>(sizeof(T)), kPieces = GT * D / kPiece;
+    static_assert(kPieces <= THREADS, "");
+    const int q_head = tid / (D / kPiece), q_piece = tid % (D / kPiece);
+    uint4 q_mine = make_uint4(0, 0, 0, 0);
+    if (q_head < heads) q_mine = *reinterpret_cast<const uint4*>(q0 + q_head * p.q_sh + q_piece * kPiece);
     int mine[kCaStages];
     int pos[kCaStages];
 #pragma unroll
@@ -835,16 +849,12 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     q_buffer ^= 1;
     if constexpr (sizeof(T) == 4) {
       float* q_shared = reinterpret_cast<float*>(ca_smem + WARPS * W::kRing) + q_buffer * (GT * (D + 4));
-      for (int i = tid; i < GT * D; i += THREADS) q_shared[i] = i / D < heads ? q0[(i / D) * p.q_sh + i % D] : 0.f;
+      if (tid < kPieces) reinterpret_cast<uint4*>(q_shared)[tid] = q_mine;
       if (POS == 2 && tid < GT) q_shared[GT * D + tid] = tid < heads ? p.slopes[hq + tid] * 1.4426950408889634f : 0.f;
       sums.start(p, q_shared, heads, hq);
     } else {
       uint8_t* q_shared = ca_smem + WARPS * W::kRing + q_buffer * (GT * Sums::kQ);
-      for (int i = tid; i < GT * D / 8; i += THREADS) {           // 16 bytes each
-        const int g = i / (D / 8), piece = i % (D / 8);
-        *reinterpret_cast<uint4*>(q_shared + g * Sums::kQ + piece * 16) =
-            g < heads ? *reinterpret_cast<const uint4*>(q0 + g * p.q_sh + piece * 8) : make_uint4(0, 0, 0, 0);
-      }
+      if (tid < kPieces) *reinterpret_cast<uint4*>(q_shared + q_head * Sums::kQ + q_piece * 16) = q_mine;
       sums.start(p, static_cast<uint32_t>(__cvta_generic_to_shared(q_shared)), heads, hq);
     }
   };
@@ -890,22 +900,23 @@ __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) 
     const int64_t head0 = (static_cast<int64_t>(was.b) * p.num_kv_heads + h_was) * p.group + (was.unit - h_was * p.head_blocks) * GT;
     // the output, or a partial result that the unit's last CTA joins with the others
     float* part = p.partials + static_cast<int64_t>(was.slot) * kCaPartial;
-    for (int o = tid; o < heads_was * D; o += THREADS) {
+    for (int o = tid * 4; o < heads_was * D; o += THREADS * 4) {
       const int g = o / D, channel = o - g * D;
       float m = s_m[0][g];
 #pragma unroll
       for (int w = 1; w < WARPS; ++w) m = fmaxf(m, s_m[w][g]);
-      float z = 0.f, a = 0.f;
+      float z = 0.f;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
         const float f = ca_factor(s_m[w][g], m);
         z = fmaf(s_z[w][g], f, z);
-        a = fmaf(reinterpret_cast<const float*>(ca_smem + w * W::kRing + kAcc)[g * W::HEAD + channel], f, a);
+        ca_add(a, *reinterpret_cast<const float4*>(ca_smem + w * W::kRing + kAcc + (g * W::HEAD + channel) * 4), f);
       }
       if (was.whole) {
         ca_write(p, head0 + g, D, channel, m, z, a);
       } else {
-        __stcg(part + o, a);
+        __stcg(reinterpret_cast<float4*>(part + o), a);
         if (channel == 0) {
           __stcg(part + GT * D + g, m);
           __stcg(part + GT * D + GT + g, z);

@@ -225,6 +225,16 @@ def test_strided_queries_and_no_lse():
     assert torch.equal(out.cpu(), want)
 
 
+def test_outputs_need_no_more_than_a_float_s_alignment():
+    for lens in ([200, 3], [6000]):                                  # whole heads, and heads that are joined
+        x = Data((8, 1), 64, "bf16", 16, lens)
+        want, want_lse = x.run()
+        flat = torch.full((len(lens) * 8 * 64 + 2,), 5.0, device=DEV)
+        out = flat[1:-1].view(len(lens), 8, 64)
+        pkv.decode_attention_cache(x.cfg, x.cache, 0, x.q.to(DEV), out, x.ws)
+        assert torch.equal(out.cpu(), want) and flat[0] == 5.0 and flat[-1] == 5.0
+
+
 def test_captured_calls_follow_the_lengths_on_the_device():
     """A graph captured once is replayed as the cache grows; calls of several sizes share the workspace, one after another."""
     x = Data((8, 2), 64, "bf16", 16, [900, 500, 64])
