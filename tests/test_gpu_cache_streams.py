@@ -231,3 +231,19 @@ def test_a_long_run_of_steps_with_nothing_waited_for(page):
                         continue
                     want, _, size = attend(q[s, l, b, hq, 0], torch.stack(ks), torch.stack(vs))
                     assert torch.all((got[s, l, b, hq].double() - want).abs() <= 1e-4 * size + 1e-7), (s, l, b, h)
+
+
+def test_the_largest_batch():
+    lens = [(7 * i) % 5 for i in range(1024)]
+    x = Data((2, 1), 64, "fp16", 2, lens)
+    out, lse = x.run(use_positions=True, window=6)
+    x.check(out, lse, use_positions=True, window=6)
+    # one sequence goes on as 1024
+    p = Pool(pkv.make_config(num_layers=1, num_q_heads=1, num_kv_heads=1, head_dim=64, window=1, pool_kernel=1, dtype="bf16", avg_budget=1), [[6, 9]], 4, 3000, 4)
+    to = p.other(1024)
+    parents, add = [1] * 600 + [0] * 400 + [-1] * 24, [[i % 3 for i in range(1024)]]
+    pkv.cache_fork(p.cfg, p.cache, add_tensor(parents), p.ws, add=add_tensor(add), to=to)
+    pkv.check_status(p.ws)
+    copies = p.lists.fork(parents, add)[1]
+    p.lists.check(to.tables.cpu(), to.lens.cpu(), to.refs.cpu())
+    p.check_pools(copies)
