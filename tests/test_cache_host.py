@@ -185,3 +185,14 @@ def test_page_calls_that_make_no_sense_are_refused():
             assert f(to=cache(**{part: P + 4096})) == INVALID
     assert reserve(to=cache(**other, batch=4)) == INVALID and compact(to=cache(**other, batch=4)) == INVALID
     assert fork(to=cache(batch=4)) == INVALID                                # in place with another batch
+
+
+def test_position_lists_that_make_no_sense_are_refused():
+    lens = (ctypes.c_int32 * 2)(40, 9)
+
+    def call_positions(cfg=None, indices=P, batch=2, k_layer=3, table=P, page=4, pages=10, positions=P, ws=P, size=256, seq=lens):
+        return call("pyramidkv_cache_positions", ctypes.byref(cfg or config()), indices, seq, batch, k_layer, table, page, pages, positions, ws, size, None)
+    for bad in (dict(indices=None), dict(table=None), dict(positions=None), dict(page=0), dict(pages=0), dict(batch=0), dict(k_layer=-1), dict(seq=None)):
+        assert call_positions(**bad) == INVALID, bad
+    assert call_positions(batch=65) == UNSUPPORTED and call_positions(cfg=config(head_dim=96)) == UNSUPPORTED
+    assert call_positions(ws=None) == WORKSPACE and call_positions(size=255) == WORKSPACE and call_positions(ws=P + 64) == WORKSPACE

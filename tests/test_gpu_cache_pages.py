@@ -310,6 +310,49 @@ def test_page_calls_need_refs_and_fitting_tensors():
             pkv.PagedCache(x.cfg, kw.pop("k_pool"), kw.pop("v_pool"), kw.pop("tables"), kw.pop("lens"), **kw)
 
 
+def test_positions_of_kept_rows_follow_the_block_table():
+    cfg = pkv.make_config(num_layers=1, num_q_heads=2, num_kv_heads=2, head_dim=64, window=4, pool_kernel=1, dtype="bf16", avg_budget=8)
+    lens, kl, page = [30, 6, 100], 9, 4
+    counts = [pkv.kept_count(cfg, kl, n) for n in lens]
+    pages = [pkv.pages_needed(cfg, kl, n, page) for n in lens]
+    g = torch.Generator().manual_seed(4)
+    table = torch.randperm(2 * sum(pages) + 3, generator=g)[:2 * sum(pages)].to(torch.int32)
+    idx = torch.cat([torch.randint(0, n, (2 * c,), generator=g) for n, c in zip(lens, counts)]).to(torch.int32)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+
+    def check(bad_pages=(), bad_rows=()):
+        t, i = table.clone(), idx.clone()
+        for e in bad_pages:
+            t[e] = 10 ** 6
+        for r in bad_rows:
+            i[r] = 100
+        got = torch.full((2 * sum(pages) + 3, page), -7, dtype=torch.int32, device=DEV)
+        want = got.cpu()
+        pkv.cache_positions(cfg, i.to(DEV), lens, kl, t.to(DEV), got, ws)
+        entry = row = 0
+        for b, c in enumerate(counts):
+            for h in range(2):
+                for r in range(c):
+                    if entry + r // page not in bad_pages and row + r not in bad_rows:
+                        want[int(table[entry + r // page]), r % page] = idx[row + r]
+                entry += pages[b]
+                row += c
+        assert torch.equal(got.cpu(), want)
+    check()
+    pkv.check_status(ws)
+    check(bad_pages=(1, len(table) - 1))
+    with pytest.raises(pkv.PkvError, match="0x4"):
+        pkv.check_status(ws)
+    ws.zero_()
+    check(bad_rows=(0, len(idx) - 1))
+    with pytest.raises(pkv.PkvError, match="0x8"):
+        pkv.check_status(ws)
+    for bad in (dict(indices=idx[:-1].to(DEV)), dict(table=table[:-1].to(DEV)), dict(positions=torch.zeros(4, page, device=DEV))):
+        with pytest.raises(ValueError):
+            kw = {**dict(indices=idx.to(DEV), table=table.to(DEV), positions=torch.zeros(99, page, dtype=torch.int32, device=DEV)), **bad}
+            pkv.cache_positions(cfg, kw["indices"], lens, kl, kw["table"], kw["positions"], ws)
+
+
 # ------------------------------------------------------------------------------------------------ all of it together
 class Rows:
     """What a sequence's head holds: (key as stored, value, position), oldest first."""
