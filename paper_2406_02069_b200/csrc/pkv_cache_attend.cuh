@@ -17,8 +17,9 @@
 //   * A warp takes tiles of 16 rows (fp32: 8), kCaStages of them in shared memory or on their way by asynchronous copies.  A row that is
 //     not seen is filled with zeros instead of read; a tile without a seen row costs its positions only.
 //   * 16-bit rows go through mma.sync, fp32 accumulation, the query heads as M: GT = 4 heads with the high, middle and low
-//     16-bit parts of their softmax weights in rows 0-3, 4-7 and 8-11, GT = 8 with high and middle parts in one product and
-//     the low ones in a second.  The parts carry 24 bits, so the weights stay fp32 in effect.
+//     16-bit parts of their softmax weights in rows 0-3, 4-7 and 8-11, GT = 8 with high and middle parts in one product (rows 0-7
+//     and 8-15) and the low ones in a second, added to the middle ones.  The parts carry the 24 bits of an fp32 weight (fp16: of
+//     weights down to 2^-27 of the largest, Dec16).
 //   * fp32 rows: a lane has a quarter of a row's dot products, then four channels of all rows; GT = 1, 2, 4 or 8.
 #pragma once
 
@@ -267,9 +268,11 @@ struct CaSums {
       z += w0 + w1;
       const uint32_t high = X::pack(w0, w1);
       const float2 hf = X::unpack(high);
-      const uint32_t mid = X::pack(w0 - hf.x, w1 - hf.y);
+      constexpr float kUp = 1 << X::kFine;
+      const float r0 = (w0 - hf.x) * kUp, r1 = (w1 - hf.y) * kUp;
+      const uint32_t mid = X::pack(r0, r1);
       const float2 mf = X::unpack(mid);
-      const uint32_t low = X::pack(w0 - hf.x - mf.x, w1 - hf.y - mf.y);
+      const uint32_t low = X::pack(r0 - mf.x, r1 - mf.y);
       if (GT == 4) {
         a[t][0] = g < 4 ? high : mid;
         a[t][1] = g < 4 ? low : 0u;
@@ -297,8 +300,8 @@ struct CaSums {
         X::mma(d0, a[0][0], a[0][1], a[1][0], a[1][1], e0, e1);
         X::mma(d1, a[0][0], a[0][1], a[1][0], a[1][1], f0, f1);
         if (GT == 8) {
-          X::mma(d0, low8[0], 0u, low8[1], 0u, e0, e1);
-          X::mma(d1, low8[0], 0u, low8[1], 0u, f0, f1);
+          X::mma(d0, 0u, low8[0], 0u, low8[1], e0, e1);
+          X::mma(d1, 0u, low8[0], 0u, low8[1], f0, f1);
         }
         unsigned long long* to = o[j * 8 + 2 * w];
         to[0] = add2(to[0], pack2(d0[0], d0[1]));
@@ -317,6 +320,13 @@ struct CaSums {
     z += __shfl_xor_sync(0xffffffffu, z, 2);
     float special = 0.f;                   // NaN once a sum is not finite
     __syncwarp();
+    // fragment rows g and g + 8 together, the middle and low parts with their factor taken off
+    constexpr float kDown = 1.f / (1 << X::kFine);
+    const float top = GT == 4 && g >= 4 ? kDown : 1.f;
+    auto join = [&](const unsigned long long (&x)[2]) {
+      if (X::kFine == 0) return add2(x[0], x[1]);
+      return fma2(x[1], pack2(kDown, kDown), mul2(x[0], pack2(top, top)));
+    };
     if (GT == 4) {
       // Lanes g and g + 4 hold parts of the same sums: each keeps one of the channel octets 64 j + 8 (2c + e) + 0 .. 7 of head g % 4
       const bool upper = g >= 4;
@@ -326,7 +336,7 @@ struct CaSums {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           float s0, s1;
-          unpack2(add2(o[j * 8 + i][0], o[j * 8 + i][1]), s0, s1);
+          unpack2(join(o[j * 8 + i]), s0, s1);
           t[i] = (upper ? s1 : s0) + __shfl_xor_sync(0xffffffffu, upper ? s0 : s1, 16);
           special = fmaf(t[i], 0.f, special);
         }
@@ -340,7 +350,7 @@ struct CaSums {
         float t[2][8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          unpack2(add2(o[j * 8 + i][0], o[j * 8 + i][1]), t[0][i], t[1][i]);
+          unpack2(join(o[j * 8 + i]), t[0][i], t[1][i]);
           special = fmaf(t[0][i], 0.f, special);
           special = fmaf(t[1][i], 0.f, special);
         }

@@ -5,11 +5,19 @@
 
 namespace pkv {
 
+// 16-bit types of the matrix products.  A softmax weight w 2^kShift (w <= 1) is taken apart into a high part and, of what that leaves
+// times 2^kFine, a middle and a low one; sums of the latter two are multiplied by 2^-kFine at the end.
+//   bfloat16: the range of fp32, so that the three parts carry 24 bits of every weight.
+//   fp16: its smallest step is 2^-24, and without a factor of their own the lower parts of small weights would be subnormal (11 bits
+//   left of a weight of 2^-27).  With 2^13 on the weight and 2^13 more on what the high part leaves (at most 2^1, so 2^14 of
+//   the largest 2^16) the parts are off by 2^-25 of the weight or 2^-51 of the largest one, whichever is more: 24 bits of weights
+//   down to 2^-27.
 template <typename T>
 struct Dec16;
 template <>
 struct Dec16<__nv_bfloat16> {
-  static constexpr float kShift = 0.f;    // bfloat16 has the range of fp32
+  static constexpr float kShift = 0.f;
+  static constexpr int kFine = 0;
   __device__ __forceinline__ static uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
@@ -25,7 +33,8 @@ struct Dec16<__nv_bfloat16> {
 };
 template <>
 struct Dec16<__half> {
-  static constexpr float kShift = 13.f;   // weights carry 2^13, so that the third part of small ones is not subnormal
+  static constexpr float kShift = 13.f;
+  static constexpr int kFine = 13;
   __device__ __forceinline__ static uint32_t pack(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
