@@ -9,8 +9,8 @@
 //     call has no workspace): the CTAs hand their sums to one another through distributed shared memory, each channel
 //     to the CTA that finishes it, with one cluster barrier.
 //   * 16-bit rows go through mma.sync (decode_mma_kernel): M = query heads, fp32 accumulation.  The softmax weights stay
-//     fp32 in effect: each is split into three 16-bit parts (hi + mid + lo carry 24 bits and more), which stand in
-//     different rows of the same M = 16 operand (4 heads x 3 parts), so that the split costs no extra products.
+//     fp32 in effect: each is split into three 16-bit parts (24 bits; fp16: of weights down to 2^-27 of the largest, Dec16),
+//     which stand in different rows of the same M = 16 operand (4 heads x 3 parts), so that the split costs no extra products.
 //     Rows come by asynchronous copies into a ring in shared memory, three tiles of 16 rows per warp: a tile in registers
 //     at a time left the warp waiting some 1.1 us for every tile, and took the registers that a second CTA on the SM needs.
 //   * fp32 rows stay on the fp32 pipe (decode_attention_kernel).
@@ -527,9 +527,11 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 1 : 2) decode_mma_ker
         z += w0 + w1;
         const uint32_t high = X::pack(w0, w1);
         const float2 hf = X::unpack(high);
-        const uint32_t mid = X::pack(w0 - hf.x, w1 - hf.y);
+        constexpr float kUp = 1 << X::kFine;
+        const float r0 = (w0 - hf.x) * kUp, r1 = (w1 - hf.y) * kUp;
+        const uint32_t mid = X::pack(r0, r1);
         const float2 mf = X::unpack(mid);
-        const uint32_t low = X::pack(w0 - hf.x - mf.x, w1 - hf.y - mf.y);
+        const uint32_t low = X::pack(r0 - mf.x, r1 - mf.y);
         a[t][0] = g < 4 ? high : mid;
         a[t][1] = g < 4 ? low : 0u;
       }
@@ -561,12 +563,15 @@ __global__ void __launch_bounds__(WARPS * 32, WARPS == 8 ? 1 : 2) decode_mma_ker
   // Lanes g and g + 4 hold parts of the same sums: each keeps one of the two channel octets 64 j + 8 (2c + e) + 0 .. 7 of head
   // g % 4, the lower one e = 0.  (Sixteen-byte stores; scalar ones met in two banks, eight lanes each, 0.7 us.)
   const bool upper = g >= 4;
+  constexpr float kDown = 1.f / (1 << X::kFine);  // the factor of middle and low parts, taken off
+  const float top = upper ? kDown : 1.f;
+  auto join = [&](float x, float y) { return X::kFine == 0 ? x + y : fmaf(y, kDown, x * top); };
 #pragma unroll
   for (int j = 0; j < VC; ++j) {
     float s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float s0 = o[j * 8 + i][0] + o[j * 8 + i][2], s1 = o[j * 8 + i][1] + o[j * 8 + i][3];
+      const float s0 = join(o[j * 8 + i][0], o[j * 8 + i][2]), s1 = join(o[j * 8 + i][1], o[j * 8 + i][3]);
       s[i] = (upper ? s1 : s0) + __shfl_xor_sync(0xffffffffu, upper ? s0 : s1, 16);
       special[i & 3] = fmaf(s[i], 0.f, special[i & 3]);
     }
