@@ -627,7 +627,10 @@ struct CaPlan {
 
   __device__ __forceinline__ int64_t start_of(int64_t cta) const { return total * cta / gridDim.x; }
   __device__ __forceinline__ int64_t owner(int64_t tile) const { return ((tile + 1) * gridDim.x - 1) / total; }
-  __device__ __forceinline__ int64_t ahead(const int32_t* off, int s) const { return static_cast<int64_t>(off[s] + kCaStart * s) * per_seq; }
+  // Counted tiles of the sequences ahead (the sum passes 2^31 where off comes near it).
+  __host__ __device__ __forceinline__ int64_t ahead(const int32_t* off, int s) const {
+    return (static_cast<int64_t>(off[s]) + int64_t{kCaStart} * s) * per_seq;
+  }
 };
 
 // The next segment of this CTA's range.  One thread.
