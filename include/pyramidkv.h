@@ -29,8 +29,9 @@
  *     launch): a kernel of the library does its set-up while its predecessor drains, and waits for the
  *     predecessor's completion before it touches global memory.  The one exception is opt-in: with
  *     PKV_FLAG_INPUTS_FINAL in cfg->flags the score kernels read q_win and k without that wait (see the
- *     flag).  Even then the library orders them itself when q_win or k lies inside a cache or page pool
- *     that one of its own recent calls writes, or is what pyramidkv_rotary has just written.
+ *     flag).  Even then the library orders them itself when q_win or k overlaps K/V rows, pages or rotated
+ *     queries and keys that a call of its own may still be writing: it remembers them until 128 launches of
+ *     its kernels have followed in their stream, which is more than a device holds at once.
  *   - Calls on different streams may run at the same time as long as each has a workspace of its own (a
  *     call keeps its intermediate results there); the layers of a model are independent of one another, so a
  *     caller may spread them over a few streams to keep the device busy during the short kernels of a layer.

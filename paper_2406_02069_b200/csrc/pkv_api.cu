@@ -497,6 +497,7 @@ int launch_scores_tc(const pkv_config* c, const pkv_tensor& q, const pkv_tensor&
              : small ? cudaLaunchKernelEx(&cfg, score_resident_kernel<D, kRsStagesShort, 2>, q_map, k_map, tp)
                      : cudaLaunchKernelEx(&cfg, score_resident_kernel<D, kRsStages, 2>, q_map, k_map, tp)) != cudaSuccess)
       return PKV_ERR_CUDA;
+    note_launch(st);
     mark(st, "scores_resident");
     return check_launch();
   }
@@ -769,16 +770,17 @@ int run_select(const pkv_config* c, const float* scores, int64_t ld, const SeqTa
   cfg.numAttrs = 2;
   void* args[1] = {&sp};
   if (cudaLaunchKernelExC(&cfg, kernel, args) != cudaSuccess) return PKV_ERR_CUDA;
+  note_launch(st);
   if (k_out && !paged) {
     int64_t out_rows = 0;
     for (int b = 0; b < batch; ++b) out_rows += static_cast<int64_t>(c->num_kv_heads) * table.count[b];
     const size_t out_bytes = static_cast<size_t>(out_rows) * c->head_dim * sp.elem_bytes;
-    note_output(k_out, out_bytes);
-    note_output(v_out, out_bytes);
+    note_output(k_out, out_bytes, st);
+    note_output(v_out, out_bytes, st);
   } else if (paged) {
     const size_t pool_bytes = static_cast<size_t>(paged->num_pages) * paged->page_size * c->head_dim * sp.elem_bytes;
-    note_output(k_out, pool_bytes);
-    note_output(v_out, pool_bytes);
+    note_output(k_out, pool_bytes, st);
+    note_output(v_out, pool_bytes, st);
   }
   mark(st, k_out ? "pool_select_gather" : "pool_select");
   return check_launch();
@@ -807,8 +809,8 @@ int run_gather(const pkv_config* c, const pkv_tensor& k, const pkv_tensor& v, co
   if (threads == 0) return PKV_OK;
   const unsigned blocks = static_cast<unsigned>((threads + kGatherThreads - 1) / kGatherThreads);
   launch_pdl(gather_rows_kernel, blocks, kGatherThreads, 0, st, gp);
-  note_output(k_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes);
-  note_output(v_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes);
+  note_output(k_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes, st);
+  note_output(v_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes, st);
   mark(st, "gather_rows");
   return check_launch();
 }
@@ -834,8 +836,8 @@ int run_gather_paged(const pkv_config* c, const pkv_tensor& k, const pkv_tensor&
   const unsigned blocks = static_cast<unsigned>((threads + kPagedThreads - 1) / kPagedThreads);
   launch_pdl(gather_paged_kernel, blocks, kPagedThreads, 0, st, gp);
   const size_t pool_bytes = static_cast<size_t>(num_pages) * page_size * c->head_dim * gp.elem_bytes;
-  note_output(k_pool, pool_bytes);
-  note_output(v_pool, pool_bytes);
+  note_output(k_pool, pool_bytes, st);
+  note_output(v_pool, pool_bytes, st);
   mark(st, "gather_paged");
   return check_launch();
 }
@@ -871,6 +873,7 @@ int launch_decode(void (*kernel)(DecodeParams), const DecodeParams& dp, int batc
   cfg.numAttrs = 2;
   void* args[1] = {const_cast<DecodeParams*>(&dp)};
   if (cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), args) != cudaSuccess) return PKV_ERR_CUDA;
+  note_launch(st);
   return check_launch();
 }
 
@@ -1498,8 +1501,8 @@ int pyramidkv_shard_gather(const pkv_config* cfg, pkv_tensor k_shard, pkv_tensor
   if (threads == 0) return PKV_OK;
   launch_pdl(gather_shard_kernel, static_cast<unsigned>((threads + kShardThreads - 1) / kShardThreads), kShardThreads,
              0, static_cast<cudaStream_t>(stream), gp);
-  note_output(k_out, static_cast<size_t>(rows) * cfg->head_dim * eb);
-  note_output(v_out, static_cast<size_t>(rows) * cfg->head_dim * eb);
+  note_output(k_out, static_cast<size_t>(rows) * cfg->head_dim * eb, static_cast<cudaStream_t>(stream));
+  note_output(v_out, static_cast<size_t>(rows) * cfg->head_dim * eb, static_cast<cudaStream_t>(stream));
   return check_launch();
 }
 

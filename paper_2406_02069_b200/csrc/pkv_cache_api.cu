@@ -98,9 +98,9 @@ size_t pool_bytes(const pkv_config* c, const pkv_cache* x) {
   return static_cast<size_t>(x->num_pages) * x->page_size * c->head_dim * elem_bytes(c);
 }
 
-void note_rows(const pkv_tensor& t, int64_t batch, int heads, int64_t tokens, int d, int elem) {
+void note_rows(const pkv_tensor& t, int64_t batch, int heads, int64_t tokens, int d, int elem, cudaStream_t st) {
   if (!t.ptr) return;
-  note_output(t.ptr, static_cast<size_t>((batch - 1) * t.stride_batch + (heads - 1) * t.stride_head + (tokens - 1) * t.stride_token + d) * elem);
+  note_output(t.ptr, static_cast<size_t>((batch - 1) * t.stride_batch + (heads - 1) * t.stride_head + (tokens - 1) * t.stride_token + d) * elem, st);
 }
 
 // ---------------------------------------------------------------- rotary positions
@@ -216,7 +216,9 @@ int launch_cluster(void (*kernel)(PagesParams), const PagesParams& p, cudaStream
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? check_launch() : PKV_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) return PKV_ERR_CUDA;
+  note_launch(st);
+  return check_launch();
 }
 
 // Blocks for a grid-stride loop over n items.
@@ -280,8 +282,8 @@ int run_fork(const pkv_config* c, const pkv_cache* from, const pkv_cache* to, Pa
   if (const int rc = launch_cluster(pages_deal_kernel, p, st)) return rc;
   if (p.parents) {
     launch_pdl(pages_copy_kernel, dim3(p.to_batch, p.layers), dim3(kPgCarryThreads), 0, st, p);
-    note_output(from->k_pool, pool_bytes(c, from));
-    note_output(from->v_pool, pool_bytes(c, from));
+    note_output(from->k_pool, pool_bytes(c, from), st);
+    note_output(from->v_pool, pool_bytes(c, from), st);
   }
   return check_launch();
 }
@@ -358,8 +360,8 @@ int pyramidkv_rotary(const pkv_config* cfg, const pkv_rotary* plan, const int32_
   p.batch = batch;
   p.tokens = tokens;
   const int st = launch_rotary<false>(cfg, plan, inverse, p, static_cast<cudaStream_t>(stream));
-  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e);
-  note_rows(k_out, batch, cfg->num_kv_heads, tokens, d, e);
+  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
+  note_rows(k_out, batch, cfg->num_kv_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
   return st;
 }
 
@@ -402,9 +404,9 @@ int pyramidkv_append_cache(const pkv_config* cfg, const pkv_cache* cache, int32_
   p.pos_pool = cache->positions;
   p.status = w.status;
   const int st = launch_rotary<true>(cfg, plan_or_null, 0, p, static_cast<cudaStream_t>(stream));
-  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e);
-  note_output(cache->k_pool, pool_bytes(cfg, cache));
-  note_output(cache->v_pool, pool_bytes(cfg, cache));
+  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
+  note_output(cache->k_pool, pool_bytes(cfg, cache), static_cast<cudaStream_t>(stream));
+  note_output(cache->v_pool, pool_bytes(cfg, cache), static_cast<cudaStream_t>(stream));
   return st;
 }
 
@@ -504,8 +506,8 @@ int pyramidkv_cache_compact(const pkv_config* cfg, const pkv_cache* from, const 
   if (const int rc = launch_cluster(pages_pair_kernel, p, st)) return rc;
   const int64_t units = static_cast<int64_t>(p.layers) * p.from_batch;
   launch_pdl(pages_move_kernel, dim3(stride_grid(std::max<int64_t>(p.num_pages / 2, units), 1, sms, 16)), dim3(kPgCopyThreads), 0, st, p);
-  note_output(from->k_pool, pool_bytes(cfg, from));
-  note_output(from->v_pool, pool_bytes(cfg, from));
+  note_output(from->k_pool, pool_bytes(cfg, from), st);
+  note_output(from->v_pool, pool_bytes(cfg, from), st);
   return check_launch();
 }
 

@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 #include <utility>
 
@@ -50,6 +51,112 @@ inline TensorView view(const pkv_tensor& t) { return TensorView{t.ptr, t.stride_
 
 inline int check_launch() { return cudaPeekAtLastError() == cudaSuccess ? PKV_OK : PKV_ERR_CUDA; }
 
+// ---------------------------------------------------------------- outputs still in flight
+// The tensor-core sweeps start reading Q and K before the kernels ahead of them in the stream have finished.
+// That is only right for tensors those kernels do not write, so the library remembers where its calls put K/V rows (packed
+// caches, page pools, rotated keys and queries) and a sweep whose Q or K overlaps one of them waits like any other kernel.
+//   How long: a kernel starts when all CTAs of the one ahead in its stream have started, and every kernel of the library stays
+// until the one ahead of it has finished.  So whatever is between a kernel that still writes and a sweep is on the device with
+// both, and a device holds kResidentGrids grids: what has as many launches behind it in its own stream is complete.  Every stream has
+// ranges of its own, since launches on another one say nothing about it; a sweep looks at all of them.
+//   A range that is written again is taken once, by its last writer; ranges whose stream makes room for another one (more than
+// kOutStreams of them) stay for good, as parts of one range.
+constexpr unsigned kResidentGrids = 128;   // compute capability 10.0
+constexpr int kOutRanges = 3 * kResidentGrids;                  // no launch has more than three outputs
+constexpr int kOutStreams = 64;
+
+struct OutputRecord {
+  struct Range { uintptr_t lo, hi; uint64_t at; };              // at: launches of the stream when it was written
+  struct Stream {
+    cudaStream_t stream;
+    int device;
+    uint64_t thread;                       // of the per-thread stream, whose handle is the same in all threads
+    uint64_t launches, used;
+    int count;
+    Range range[kOutRanges];
+    bool live(const Range& r) const { return launches - r.at < kResidentGrids; }
+  };
+  std::mutex mutex;
+  Stream streams[kOutStreams];
+  int known = 0;
+  uint64_t clock = 0;
+  Range rest = {};                         // hi 0: none
+
+  static uint64_t this_thread() {
+    static std::atomic<uint64_t> next{1};
+    static thread_local const uint64_t id = next.fetch_add(1);
+    return id;
+  }
+  void stays(const Range& r) {
+    rest.lo = rest.hi ? std::min(rest.lo, r.lo) : r.lo;
+    rest.hi = std::max(rest.hi, r.hi);
+  }
+  Stream& of(cudaStream_t st) {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+    const uint64_t thread = st == cudaStreamPerThread ? this_thread() : 0;
+    ++clock;
+    Stream* oldest = streams;
+    for (int i = 0; i < known; ++i) {
+      Stream& s = streams[i];
+      if (s.stream == st && s.device == dev && s.thread == thread) {
+        s.used = clock;
+        return s;
+      }
+      if (s.used < oldest->used) oldest = &s;
+    }
+    Stream& s = known < kOutStreams ? streams[known++] : *oldest;
+    for (int i = 0; i < s.count; ++i)
+      if (s.live(s.range[i])) stays(s.range[i]);
+    s.stream = st;
+    s.device = dev;
+    s.thread = thread;
+    s.launches = 0;
+    s.used = clock;
+    s.count = 0;
+    return s;
+  }
+  void launched(cudaStream_t st) {
+    std::lock_guard<std::mutex> lock(mutex);
+    ++of(st).launches;
+  }
+  void wrote(const void* ptr, size_t bytes, cudaStream_t st) {
+    if (!ptr || !bytes) return;
+    std::lock_guard<std::mutex> lock(mutex);
+    Stream& s = of(st);
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(ptr), hi = lo + bytes;
+    int n = 0;
+    for (int i = 0; i < s.count; ++i) {    // what is complete goes, and what this range takes in
+      const Range r = s.range[i];
+      if (s.live(r) && !(lo <= r.lo && r.hi <= hi)) s.range[n++] = r;
+    }
+    if (n == kOutRanges) stays(s.range[--n]);
+    s.range[n] = Range{lo, hi, s.launches};
+    s.count = n + 1;
+  }
+  bool overlaps(uintptr_t lo, uintptr_t hi) {
+    std::lock_guard<std::mutex> lock(mutex);
+    if (lo < rest.hi && rest.lo < hi) return true;
+    for (int i = 0; i < known; ++i)
+      for (int j = 0; j < streams[i].count; ++j) {
+        const Range& r = streams[i].range[j];
+        if (lo < r.hi && r.lo < hi && streams[i].live(r)) return true;
+      }
+    return false;
+  }
+};
+inline OutputRecord g_outputs;
+
+inline void note_launch(cudaStream_t st) { g_outputs.launched(st); }
+inline void note_output(const void* ptr, size_t bytes, cudaStream_t st) { g_outputs.wrote(ptr, bytes, st); }
+
+inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {
+  const int64_t last = (batch - 1) * std::max<int64_t>(t.stride_batch, 0) +
+                       (heads - 1) * std::max<int64_t>(t.stride_head, 0) + (tokens - 1) * t.stride_token + d;
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(t.ptr), hi = lo + static_cast<uintptr_t>(last) * elem_bytes;
+  return g_outputs.overlaps(lo, hi);
+}
+
 // Launch with programmatic stream serialisation: the kernel may be scheduled while its predecessor in
 // the stream drains; the kernels order themselves with pdl_wait() (pkv_common.cuh).
 template <typename... KArgs, typename... Args>
@@ -64,34 +171,7 @@ void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cu
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
-}
-
-// ---------------------------------------------------------------- outputs still in flight
-// The tensor-core sweeps start reading Q and K before the kernels ahead of them in the stream have finished.
-// That is only right for tensors those kernels do not write, so the library remembers where its last calls put
-// K/V rows (packed caches, page pools, rotated keys and queries) and a sweep whose Q or K overlaps one of them waits like any other kernel.
-struct ByteRange { uintptr_t lo, hi; };
-inline std::mutex g_out_mutex;
-constexpr unsigned kRecentOut = 256;       // a kernel can wait behind as many as fit on the device at once
-inline ByteRange g_recent_out[kRecentOut];
-inline unsigned g_recent_out_next = 0;
-
-inline void note_output(const void* ptr, size_t bytes) {
-  if (!ptr || !bytes) return;
-  std::lock_guard<std::mutex> lock(g_out_mutex);
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(ptr);
-  g_recent_out[g_recent_out_next++ % kRecentOut] = ByteRange{lo, lo + bytes};
-}
-
-inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {
-  const int64_t last = (batch - 1) * std::max<int64_t>(t.stride_batch, 0) +
-                       (heads - 1) * std::max<int64_t>(t.stride_head, 0) + (tokens - 1) * t.stride_token + d;
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(t.ptr), hi = lo + static_cast<uintptr_t>(last) * elem_bytes;
-  std::lock_guard<std::mutex> lock(g_out_mutex);
-  for (const ByteRange& r : g_recent_out)
-    if (r.hi > r.lo && lo < r.hi && r.lo < hi) return true;
-  return false;
+  if (cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) == cudaSuccess) note_launch(st);
 }
 
 // SMs the persistent score kernels may count on: the device's, or fewer while a call runs them on a lane that
