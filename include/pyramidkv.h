@@ -695,8 +695,10 @@ int pyramidkv_decode_attention_cache(const pkv_config* cfg, const pkv_cache* cac
 /*
  * Pages.  `from` and `to` describe the same pools (equal pool pointers, positions, num_pages and page_size, layers and
  * max_pages); their tables, lens and refs are either all the same (the cache is changed in place) or all distinct.  Then
- * `from` is left as it was, except that pages it does not name may hold new rows; from that call on it is `to` that owns
- * the pool (its refs are the ones that count), and `from` is a record of the past.
+ * `from`'s arrays are left as they were, and so are the rows of its sequences that some sequence of `to` goes on with.  Pages that
+ * it does not name may hold new rows, and so may, once a fork was met, the pages of its other sequences: the fork frees them and
+ * may deal them out again itself.  From that call on it is `to` that owns the pool (its refs are the ones that count), and `from`
+ * is a record of the past.
  * All or nothing: where the pool has too few free pages, a sequence would need more than max_pages, or a parent is outside
  * [-1, batch of from), no page is dealt out or copied, granted is filled with zeros and the status word gets bit 4 (bit 3
  * for a parent).  In place everything stays as it was; a `to` of its own is not to be used then, `from` is as good as before.

@@ -315,7 +315,9 @@ def cache_fork(cfg: PkvConfig, cache: PagedCache, parents: torch.Tensor, workspa
                granted: Optional[torch.Tensor] = None, to: Optional[PagedCache] = None, stream=None) -> None:
     """Sequence c goes on from sequence parents[c] (int32), or starts empty for -1: full pages are shared, a part-filled last page
     is copied for every child behind the first, pages that nobody goes on with are freed, and add more rows are made room
-    for as by cache_reserve.  to: another cache over the same pools, with any number of sequences; None: in place."""
+    for as by cache_reserve.  to: another cache over the same pools, with any number of sequences; None: in place.  With another
+    one the parents' rows can still be read through `cache`; those of sequences that nobody goes on with cannot, their pages
+    may hold other rows already."""
     st = _native.cache_fork(cfg, getattr(cache, "struct", None), getattr(cache if to is None else to, "struct", None), parents, add, granted, workspace, stream)
     if st != _NOT_TAKEN:
         _check(st, "pyramidkv_cache_fork")
