@@ -443,6 +443,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[4] != Py_None && (!c.rows(a[4], &k, batch, c.cfg->num_kv_heads, tokens) || !c.rows(a[6], &ko, batch, c.cfg->num_kv_heads, tokens))) return not_taken();
   if (!c.on_stream(a[8])) return not_taken();
   const int inverse = PyObject_IsTrue(a[7]);
+  if (inverse < 0) { PyErr_Clear(); return not_taken(); }
   return without_gil([&] {
     return pyramidkv_rotary(c.cfg, c.plan, ints(pos), stride, static_cast<int32_t>(batch), static_cast<int32_t>(tokens), c.strided(q), c.strided(qo),
                             c.strided(k), c.strided(ko), inverse, c.stream);

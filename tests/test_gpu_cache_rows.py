@@ -187,3 +187,12 @@ def test_rotation_without_the_native_half_gives_the_same_bits(inverse, monkeypat
     assert all(torch.equal(a, b) for a, b in zip(*got)) and not torch.equal(got[0][0], q)
     with pytest.raises(ValueError):
         pkv.rotary(cfg, plan, positions[:1], q)
+
+
+def test_a_direction_that_is_neither_true_nor_false_is_refused():
+    cfg, plan = config(1, 64, "bf16"), pkv.make_rotary(64)
+    q = torch.randn(1, 1, 3, 64, device=DEV).to(torch.bfloat16)
+    before, positions = q.clone(), torch.arange(3, dtype=torch.int32, device=DEV)[None]
+    with pytest.raises(RuntimeError, match="ambiguous"):
+        pkv.rotary(cfg, plan, positions, q, inverse=torch.tensor([True, False]))
+    assert torch.equal(q, before)
