@@ -775,12 +775,10 @@ int run_select(const pkv_config* c, const float* scores, int64_t ld, const SeqTa
     int64_t out_rows = 0;
     for (int b = 0; b < batch; ++b) out_rows += static_cast<int64_t>(c->num_kv_heads) * table.count[b];
     const size_t out_bytes = static_cast<size_t>(out_rows) * c->head_dim * sp.elem_bytes;
-    note_output(k_out, out_bytes, st);
-    note_output(v_out, out_bytes, st);
+    note_outputs(st, {{k_out, out_bytes}, {v_out, out_bytes}});
   } else if (paged) {
     const size_t pool_bytes = static_cast<size_t>(paged->num_pages) * paged->page_size * c->head_dim * sp.elem_bytes;
-    note_output(k_out, pool_bytes, st);
-    note_output(v_out, pool_bytes, st);
+    note_outputs(st, {{k_out, pool_bytes}, {v_out, pool_bytes}});
   }
   mark(st, k_out ? "pool_select_gather" : "pool_select");
   return check_launch();
@@ -809,8 +807,8 @@ int run_gather(const pkv_config* c, const pkv_tensor& k, const pkv_tensor& v, co
   if (threads == 0) return PKV_OK;
   const unsigned blocks = static_cast<unsigned>((threads + kGatherThreads - 1) / kGatherThreads);
   launch_pdl(gather_rows_kernel, blocks, kGatherThreads, 0, st, gp);
-  note_output(k_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes, st);
-  note_output(v_out, static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes, st);
+  const size_t out_bytes = static_cast<size_t>(total_rows) * c->head_dim * gp.elem_bytes;
+  note_outputs(st, {{k_out, out_bytes}, {v_out, out_bytes}});
   mark(st, "gather_rows");
   return check_launch();
 }
@@ -836,8 +834,7 @@ int run_gather_paged(const pkv_config* c, const pkv_tensor& k, const pkv_tensor&
   const unsigned blocks = static_cast<unsigned>((threads + kPagedThreads - 1) / kPagedThreads);
   launch_pdl(gather_paged_kernel, blocks, kPagedThreads, 0, st, gp);
   const size_t pool_bytes = static_cast<size_t>(num_pages) * page_size * c->head_dim * gp.elem_bytes;
-  note_output(k_pool, pool_bytes, st);
-  note_output(v_pool, pool_bytes, st);
+  note_outputs(st, {{k_pool, pool_bytes}, {v_pool, pool_bytes}});
   mark(st, "gather_paged");
   return check_launch();
 }
@@ -1501,8 +1498,8 @@ int pyramidkv_shard_gather(const pkv_config* cfg, pkv_tensor k_shard, pkv_tensor
   if (threads == 0) return PKV_OK;
   launch_pdl(gather_shard_kernel, static_cast<unsigned>((threads + kShardThreads - 1) / kShardThreads), kShardThreads,
              0, static_cast<cudaStream_t>(stream), gp);
-  note_output(k_out, static_cast<size_t>(rows) * cfg->head_dim * eb, static_cast<cudaStream_t>(stream));
-  note_output(v_out, static_cast<size_t>(rows) * cfg->head_dim * eb, static_cast<cudaStream_t>(stream));
+  const size_t out_bytes = static_cast<size_t>(rows) * cfg->head_dim * eb;
+  note_outputs(static_cast<cudaStream_t>(stream), {{k_out, out_bytes}, {v_out, out_bytes}});
   return check_launch();
 }
 

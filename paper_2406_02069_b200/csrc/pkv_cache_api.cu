@@ -98,9 +98,8 @@ size_t pool_bytes(const pkv_config* c, const pkv_cache* x) {
   return static_cast<size_t>(x->num_pages) * x->page_size * c->head_dim * elem_bytes(c);
 }
 
-void note_rows(const pkv_tensor& t, int64_t batch, int heads, int64_t tokens, int d, int elem, cudaStream_t st) {
-  if (!t.ptr) return;
-  note_output(t.ptr, static_cast<size_t>((batch - 1) * t.stride_batch + (heads - 1) * t.stride_head + (tokens - 1) * t.stride_token + d) * elem, st);
+Output rows_of(const pkv_tensor& t, int64_t batch, int heads, int64_t tokens, int d, int elem) {
+  return {t.ptr, static_cast<size_t>((batch - 1) * t.stride_batch + (heads - 1) * t.stride_head + (tokens - 1) * t.stride_token + d) * elem};
 }
 
 // ---------------------------------------------------------------- rotary positions
@@ -282,8 +281,7 @@ int run_fork(const pkv_config* c, const pkv_cache* from, const pkv_cache* to, Pa
   if (const int rc = launch_cluster(pages_deal_kernel, p, st)) return rc;
   if (p.parents) {
     launch_pdl(pages_copy_kernel, dim3(p.to_batch, p.layers), dim3(kPgCarryThreads), 0, st, p);
-    note_output(from->k_pool, pool_bytes(c, from), st);
-    note_output(from->v_pool, pool_bytes(c, from), st);
+    note_outputs(st, {{from->k_pool, pool_bytes(c, from)}, {from->v_pool, pool_bytes(c, from)}});
   }
   return check_launch();
 }
@@ -360,8 +358,8 @@ int pyramidkv_rotary(const pkv_config* cfg, const pkv_rotary* plan, const int32_
   p.batch = batch;
   p.tokens = tokens;
   const int st = launch_rotary<false>(cfg, plan, inverse, p, static_cast<cudaStream_t>(stream));
-  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
-  note_rows(k_out, batch, cfg->num_kv_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
+  note_outputs(static_cast<cudaStream_t>(stream),
+               {rows_of(q_out, batch, cfg->num_q_heads, tokens, d, e), rows_of(k_out, batch, cfg->num_kv_heads, tokens, d, e)});
   return st;
 }
 
@@ -404,9 +402,8 @@ int pyramidkv_append_cache(const pkv_config* cfg, const pkv_cache* cache, int32_
   p.pos_pool = cache->positions;
   p.status = w.status;
   const int st = launch_rotary<true>(cfg, plan_or_null, 0, p, static_cast<cudaStream_t>(stream));
-  note_rows(q_out, batch, cfg->num_q_heads, tokens, d, e, static_cast<cudaStream_t>(stream));
-  note_output(cache->k_pool, pool_bytes(cfg, cache), static_cast<cudaStream_t>(stream));
-  note_output(cache->v_pool, pool_bytes(cfg, cache), static_cast<cudaStream_t>(stream));
+  note_outputs(static_cast<cudaStream_t>(stream), {rows_of(q_out, batch, cfg->num_q_heads, tokens, d, e),
+                                                   {cache->k_pool, pool_bytes(cfg, cache)}, {cache->v_pool, pool_bytes(cfg, cache)}});
   return st;
 }
 
@@ -506,8 +503,7 @@ int pyramidkv_cache_compact(const pkv_config* cfg, const pkv_cache* from, const 
   if (const int rc = launch_cluster(pages_pair_kernel, p, st)) return rc;
   const int64_t units = static_cast<int64_t>(p.layers) * p.from_batch;
   launch_pdl(pages_move_kernel, dim3(stride_grid(std::max<int64_t>(p.num_pages / 2, units), 1, sms, 16)), dim3(kPgCopyThreads), 0, st, p);
-  note_output(from->k_pool, pool_bytes(cfg, from), st);
-  note_output(from->v_pool, pool_bytes(cfg, from), st);
+  note_outputs(st, {{from->k_pool, pool_bytes(cfg, from)}, {from->v_pool, pool_bytes(cfg, from)}});
   return check_launch();
 }
 

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 #include <mutex>
 #include <utility>
 
@@ -65,6 +66,8 @@ constexpr unsigned kResidentGrids = 128;   // compute capability 10.0
 constexpr int kOutRanges = 3 * kResidentGrids;                  // no launch has more than three outputs
 constexpr int kOutStreams = 64;
 
+struct Output { const void* ptr; size_t bytes; };
+
 struct OutputRecord {
   struct Range { uintptr_t lo, hi; uint64_t at; };              // at: launches of the stream when it was written
   struct Stream {
@@ -92,8 +95,8 @@ struct OutputRecord {
     rest.hi = std::max(rest.hi, r.hi);
   }
   Stream& of(cudaStream_t st) {
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+    int dev = -1;                          // only the default streams have the same handles on all devices
+    if (reinterpret_cast<uintptr_t>(st) <= reinterpret_cast<uintptr_t>(cudaStreamPerThread) && cudaGetDevice(&dev) != cudaSuccess) dev = -1;
     const uint64_t thread = st == cudaStreamPerThread ? this_thread() : 0;
     ++clock;
     Stream* oldest = streams;
@@ -120,11 +123,13 @@ struct OutputRecord {
     std::lock_guard<std::mutex> lock(mutex);
     ++of(st).launches;
   }
-  void wrote(const void* ptr, size_t bytes, cudaStream_t st) {
-    if (!ptr || !bytes) return;
+  void wrote(cudaStream_t st, std::initializer_list<Output> outputs) {
     std::lock_guard<std::mutex> lock(mutex);
     Stream& s = of(st);
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(ptr), hi = lo + bytes;
+    for (const Output& o : outputs)
+      if (o.ptr && o.bytes) wrote(s, reinterpret_cast<uintptr_t>(o.ptr), reinterpret_cast<uintptr_t>(o.ptr) + o.bytes);
+  }
+  void wrote(Stream& s, uintptr_t lo, uintptr_t hi) {
     int n = 0;
     for (int i = 0; i < s.count; ++i) {    // what is complete goes, and what this range takes in
       const Range r = s.range[i];
@@ -148,7 +153,7 @@ struct OutputRecord {
 inline OutputRecord g_outputs;
 
 inline void note_launch(cudaStream_t st) { g_outputs.launched(st); }
-inline void note_output(const void* ptr, size_t bytes, cudaStream_t st) { g_outputs.wrote(ptr, bytes, st); }
+inline void note_outputs(cudaStream_t st, std::initializer_list<Output> outputs) { g_outputs.wrote(st, outputs); }
 
 inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {
   const int64_t last = (batch - 1) * std::max<int64_t>(t.stride_batch, 0) +

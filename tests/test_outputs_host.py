@@ -16,6 +16,7 @@ static cudaStream_t stream(uintptr_t i) { return reinterpret_cast<cudaStream_t>(
 static void* at(uintptr_t a) { return reinterpret_cast<void*>(a); }
 static bool known(uintptr_t lo, uintptr_t hi) { return g_outputs.overlaps(lo, hi); }
 static void want(bool ok, const char* what) { if (!ok) { std::printf("%s\n", what); failed = 1; } }
+static void note_output(const void* p, size_t n, cudaStream_t st) { note_outputs(st, {{p, n}}); }
 static void launch(cudaStream_t st, int n = 1) { for (int i = 0; i < n; ++i) note_launch(st); }
 int main() {
   const cudaStream_t a = stream(1), b = stream(2);
