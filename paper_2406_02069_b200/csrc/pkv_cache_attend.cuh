@@ -3,10 +3,11 @@
 //
 //   s = q . k_r scale,   x = cap tanh(s / cap) - slope_g (p - p_r),   row seen if p_r <= p and (p - p_r < window or p_r < prefix)
 //
-// What bounds it: every seen row is read once, 2 d elements for 4 d operations per query head, so the floor is the bytes of
-// the cache over the memory bandwidth (64 sequences of 129 to 4096 rows, 32 / 8 heads, bf16: 93 us, 89 % of the rate of a copy;
-// 131072 rows of one: 98, 83 %); a call with few rows is a chain of latencies (64 rows: 5.4 us, of which lengths and plan 1.5,
-// table and queries 0.7, rows and products 1.0, merge and output 0.6; 512 rows in eight parts: 8.2).
+// What bounds it: every seen row is read once for eight query heads at most, 2 d elements for 4 d operations per head, so the floor is
+// the bytes of the cache over the memory bandwidth (64 sequences of 129 to 4096 rows, 32 / 8 heads, bf16: 93 us, 89 % of the rate of
+// a copy; 131072 rows of one, 64 / 8 heads: 99, 83 %).  Sixteen query heads to a KV head are two blocks, each with its own loads: 142
+// us for 131072 rows, 128 / 8 heads.  A call with few rows is a chain of latencies (64 rows: 5.2 us, of which lengths and plan
+// 1.5, table and queries 0.7, rows and products 1.0, merge and output 0.6; 512 rows in eight parts: 8.2).
 //   * The lengths are not known on the host, so the grid does not depend on them: as many CTAs as fit on the device at once,
 //     which deal the batch's tiles (64 rows of one KV head and block of query heads) out among themselves (CaPlan).  A long
 //     sequence is split over many CTAs, and a CTA takes many short ones in turn, the next one's rows on their way while
@@ -189,7 +190,7 @@ struct CaSums {
   uint32_t q;
   // [channel octet's element][fragment rows g, g + 8]: channels of two of the octets.  Each tile's products are added to
   // them on the fp32 pipe, which rounds to nearest; the tensor core's own accumulation cuts off, and over 131072 rows that
-  // came to 2e-6 of the output (4e-7 this way).
+  // came to 2e-6 of the output (2.2e-7 this way).
   unsigned long long o[VC * 8][2];
   float m, z;                              // of head g % GT: m over the warp's rows, z over this lane's
   float slope;
@@ -746,8 +747,8 @@ __device__ __noinline__ void ca_plan(const int32_t* off, int batch, int per_seq,
   }
 }
 
-// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory: a ring per warp (+ twice GT * (D + 4)
-// floats in fp32).
+// grid: any number of CTAs up to kCaMaxGrid; block kCaThreads; dynamic shared memory: a ring per warp, and twice a segment's
+// queries (GT rows of 2 D + 64 bytes; fp32: GT * (D + 4) floats, slopes behind them).
 template <typename T, int D, int GT, int POS>
 __global__ void __launch_bounds__(kCaThreads<T>, sizeof(T) == 4 ? 1 : kCaPerSm) cache_attend_kernel(const __grid_constant__ CacheAttendParams p) {
   using W = CaWarp<T, D, GT, POS>;

@@ -1,7 +1,10 @@
 // Pages of a growing cache: room for new rows, sequences that go on from others, and pages moved together.
 //
 // A page is free if no table entry names it (refs[page] == 0).  New pages are the lowest free ones in ascending order, dealt to
-// the requests in the order (layer, sequence, head, page), so the outcome depends on nothing but the inputs.  Three kernels:
+// the requests in the order (layer, sequence, head, page), so the outcome depends on nothing but the inputs.  The kernels:
+//   0. where sequences change places: pages_stage_kernel (in place) sets all arrays aside, pages_refs_kernel (into other arrays)
+//      copies refs, ahead of step 1, which adjusts them.  Staging goes by the width of the tables, whatever the lengths (8
+//      sequences x 32 layers x 8 heads, 13 pages at most each: tables 14 pages wide 14 us for the whole fork, 8192 wide 50).
 //   1. pages_carry_kernel   (`to` is another set of arrays, or sequences change places) tables, lens and refs of `to` from those
 //      of `from`, counts of shared pages adjusted.  Grid over the table, bound by its bytes.
 //   2. pages_deal_kernel / pages_pair_kernel   one cluster of 8 CTAs, because every page's place depends on all pages below it:
@@ -46,7 +49,6 @@ struct PagesParams {
   int32_t* granted;                        // [layers][to_batch], or null
   int32_t* used;                           // compaction, or null
   int32_t layers, from_batch, to_batch, num_kv_heads, max_pages, page_size, num_pages;
-  int32_t carry;                           // step 1 runs
   int32_t in_place;
   int32_t row_pieces;                      // 16-byte pieces of a row
   uint32_t* status;

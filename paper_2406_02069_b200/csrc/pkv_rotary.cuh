@@ -7,10 +7,10 @@
 //   * The angle is formed in turns and in fp64, p * (f / 2 pi), and loses its whole turns there: in fp32 a position of 100000
 //     would leave an error of 4e-3 rad.  sincospif then sees at most half a turn.
 //   * VEC elements make 16 bytes where the pieces of the rotated part start at multiples of 16 bytes; a rotated part of another
-//     size is taken two pairs at a time (8192 tokens of 40 heads, 20 of 128 elements rotated: 43 us, 59 % of the rate of a copy), or
-//     pair by pair (61 us).
+//     size is taken two pairs at a time (8192 tokens of 40 heads, 20 of 128 elements rotated: 44 us, 59 % of the rate of a copy), or
+//     pair by pair (18 of 128: 64 us, 40 %).
 //   * 16-bit elements are taken apart and put together two to a word (one by one: 185 us for 32 / 8 heads x 32768 tokens, this way
-//     105, 98 % of the rate of a copy).  The rows come while the sines are formed, and while the page tables are read.
+//     105, 98 % of the rate of a copy; in fp32 206, 99 %).  The rows come while the sines are formed, and while the page tables are read.
 #pragma once
 
 #include "pkv_common.cuh"
