@@ -433,8 +433,8 @@ int launch_scores_tc(const pkv_config* c, const pkv_tensor& q, const pkv_tensor&
   // An early start needs the caller's word that nothing on the stream still writes Q or K, and the library's own
   // knowledge that none of its recent outputs is among them.
   tp.early = (c->flags & PKV_FLAG_INPUTS_FINAL) != 0 &&
-             !(overlaps_recent_output(q, batch, c->num_q_heads, c->window, D, 2) ||
-               overlaps_recent_output(k, batch, c->num_kv_heads, max_n, D, 2));
+             !(overlaps_recent_output(q, batch, c->num_q_heads, c->window, D, 2, st) ||
+               overlaps_recent_output(k, batch, c->num_kv_heads, max_n, D, 2, st));
   tp.prefetch_tiles = kTcPrefetchBytes / (kTcTileKeys * D * 2);
   const long long test_wait = g_test_wait_clocks.load();
   tp.wait_clocks = test_wait > 0 ? test_wait : kTcWaitCycles;

@@ -132,7 +132,8 @@ void launch_rotary_units(RotaryParams& p, int d, cudaStream_t st) {
     splits = (heads + p.head_lanes - 1) / p.head_lanes;
   }
   const int block_tokens = room / p.head_lanes;
-  launch_pdl(rotary_kernel<T, VEC, APPEND>, dim3(static_cast<unsigned>((tokens + block_tokens - 1) / block_tokens), splits), dim3(kRotThreads), 0, st, p);
+  // (counted with the outputs: a call of few rows is bound by its host time)
+  launch_uncounted(rotary_kernel<T, VEC, APPEND>, dim3(static_cast<unsigned>((tokens + block_tokens - 1) / block_tokens), splits), dim3(kRotThreads), 0, st, p);
 }
 
 template <typename T, bool APPEND>
@@ -359,7 +360,7 @@ int pyramidkv_rotary(const pkv_config* cfg, const pkv_rotary* plan, const int32_
   p.tokens = tokens;
   const int st = launch_rotary<false>(cfg, plan, inverse, p, static_cast<cudaStream_t>(stream));
   note_outputs(static_cast<cudaStream_t>(stream),
-               {rows_of(q_out, batch, cfg->num_q_heads, tokens, d, e), rows_of(k_out, batch, cfg->num_kv_heads, tokens, d, e)});
+               {rows_of(q_out, batch, cfg->num_q_heads, tokens, d, e), rows_of(k_out, batch, cfg->num_kv_heads, tokens, d, e)}, st == PKV_OK);
   return st;
 }
 
@@ -403,7 +404,7 @@ int pyramidkv_append_cache(const pkv_config* cfg, const pkv_cache* cache, int32_
   p.status = w.status;
   const int st = launch_rotary<true>(cfg, plan_or_null, 0, p, static_cast<cudaStream_t>(stream));
   note_outputs(static_cast<cudaStream_t>(stream), {rows_of(q_out, batch, cfg->num_q_heads, tokens, d, e),
-                                                   {cache->k_pool, pool_bytes(cfg, cache)}, {cache->v_pool, pool_bytes(cfg, cache)}});
+                                                   {cache->k_pool, pool_bytes(cfg, cache)}, {cache->v_pool, pool_bytes(cfg, cache)}}, st == PKV_OK);
   return st;
 }
 

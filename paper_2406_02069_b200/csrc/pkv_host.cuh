@@ -60,6 +60,8 @@ inline int check_launch() { return cudaPeekAtLastError() == cudaSuccess ? PKV_OK
 // until the one ahead of it has finished.  So whatever is between a kernel that still writes and a sweep is on the device with
 // both, and a device holds kResidentGrids grids: what has as many launches behind it in its own stream is complete.  Every stream has
 // ranges of its own, since launches on another one say nothing about it; a sweep looks at all of them.
+// Launches that are captured into a graph run later, and a graph's start waits for all that is ahead of it in the stream as
+// what follows waits for its end: a capture keeps a record of its own, and only its own sweeps look at it.
 //   A range that is written again is taken once, by its last writer; ranges whose stream makes room for another one (more than
 // kOutStreams of them) stay for good, as parts of one range.
 constexpr unsigned kResidentGrids = 128;   // compute capability 10.0
@@ -68,12 +70,30 @@ constexpr int kOutStreams = 64;
 
 struct Output { const void* ptr; size_t bytes; };
 
+struct StreamKey {
+  cudaStream_t stream;
+  int device;                              // of a default stream, whose handle is the same on all devices
+  uint64_t thread;                         // of the per-thread one, whose handle is the same in all threads
+  uint64_t capture;                        // 0: not being captured
+};
+
+inline StreamKey stream_key(cudaStream_t st) {
+  static std::atomic<uint64_t> next_thread{1};
+  static thread_local const uint64_t this_thread = next_thread.fetch_add(1);
+  StreamKey k{st, -1, st == cudaStreamPerThread ? this_thread : 0, 0};
+  if (reinterpret_cast<uintptr_t>(st) <= reinterpret_cast<uintptr_t>(cudaStreamPerThread) && cudaGetDevice(&k.device) != cudaSuccess) k.device = -1;
+  if (st && st != cudaStreamLegacy) {      // (that one cannot be captured)
+    cudaStreamCaptureStatus status;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo(st, &status, &id) == cudaSuccess && status == cudaStreamCaptureStatusActive) k.capture = id;
+  }
+  return k;
+}
+
 struct OutputRecord {
   struct Range { uintptr_t lo, hi; uint64_t at; };              // at: launches of the stream when it was written
   struct Stream {
-    cudaStream_t stream;
-    int device;
-    uint64_t thread;                       // of the per-thread stream, whose handle is the same in all threads
+    StreamKey key;
     uint64_t launches, used;
     int count;
     Range range[kOutRanges];
@@ -83,49 +103,48 @@ struct OutputRecord {
   Stream streams[kOutStreams];
   int known = 0;
   uint64_t clock = 0;
-  Range rest = {};                         // hi 0: none
+  Range rest[2] = {};                      // without and with a capture; hi 0: none
 
-  static uint64_t this_thread() {
-    static std::atomic<uint64_t> next{1};
-    static thread_local const uint64_t id = next.fetch_add(1);
-    return id;
+  void stays(const Stream& s, const Range& r) {
+    Range& to = rest[s.key.capture != 0];
+    to.lo = to.hi ? std::min(to.lo, r.lo) : r.lo;
+    to.hi = std::max(to.hi, r.hi);
   }
-  void stays(const Range& r) {
-    rest.lo = rest.hi ? std::min(rest.lo, r.lo) : r.lo;
-    rest.hi = std::max(rest.hi, r.hi);
-  }
-  Stream& of(cudaStream_t st) {
-    int dev = -1;                          // only the default streams have the same handles on all devices
-    if (reinterpret_cast<uintptr_t>(st) <= reinterpret_cast<uintptr_t>(cudaStreamPerThread) && cudaGetDevice(&dev) != cudaSuccess) dev = -1;
-    const uint64_t thread = st == cudaStreamPerThread ? this_thread() : 0;
+  Stream& of(const StreamKey& k) {
     ++clock;
+    Stream* at = nullptr;
     Stream* oldest = streams;
-    for (int i = 0; i < known; ++i) {
+    for (int i = 0; i < known && !at; ++i) {
       Stream& s = streams[i];
-      if (s.stream == st && s.device == dev && s.thread == thread) {
-        s.used = clock;
-        return s;
+      if (s.key.stream == k.stream && s.key.device == k.device && s.key.thread == k.thread && !s.key.capture == !k.capture) {
+        if (s.key.capture == k.capture) {
+          s.used = clock;
+          return s;
+        }
+        at = &s;                           // a stream is in one capture at a time: the one ahead has ended
       }
       if (s.used < oldest->used) oldest = &s;
     }
-    Stream& s = known < kOutStreams ? streams[known++] : *oldest;
-    for (int i = 0; i < s.count; ++i)
-      if (s.live(s.range[i])) stays(s.range[i]);
-    s.stream = st;
-    s.device = dev;
-    s.thread = thread;
-    s.launches = 0;
-    s.used = clock;
-    s.count = 0;
-    return s;
+    if (!at) {
+      at = known < kOutStreams ? &streams[known++] : oldest;
+      for (int i = 0; i < at->count; ++i)
+        if (at->live(at->range[i])) stays(*at, at->range[i]);
+    }
+    at->key = k;
+    at->launches = 0;
+    at->used = clock;
+    at->count = 0;
+    return *at;
   }
-  void launched(cudaStream_t st) {
+  void launched(const StreamKey& k) {
     std::lock_guard<std::mutex> lock(mutex);
-    ++of(st).launches;
+    ++of(k).launches;
   }
-  void wrote(cudaStream_t st, std::initializer_list<Output> outputs) {
+  // launches: of those that wrote, how many have not been counted
+  void wrote(const StreamKey& k, std::initializer_list<Output> outputs, int launches = 0) {
     std::lock_guard<std::mutex> lock(mutex);
-    Stream& s = of(st);
+    Stream& s = of(k);
+    s.launches += launches;
     for (const Output& o : outputs)
       if (o.ptr && o.bytes) wrote(s, reinterpret_cast<uintptr_t>(o.ptr), reinterpret_cast<uintptr_t>(o.ptr) + o.bytes);
   }
@@ -135,37 +154,40 @@ struct OutputRecord {
       const Range r = s.range[i];
       if (s.live(r) && !(lo <= r.lo && r.hi <= hi)) s.range[n++] = r;
     }
-    if (n == kOutRanges) stays(s.range[--n]);
+    if (n == kOutRanges) stays(s, s.range[--n]);
     s.range[n] = Range{lo, hi, s.launches};
     s.count = n + 1;
   }
-  bool overlaps(uintptr_t lo, uintptr_t hi) {
+  bool overlaps(uint64_t capture, uintptr_t lo, uintptr_t hi) {
     std::lock_guard<std::mutex> lock(mutex);
-    if (lo < rest.hi && rest.lo < hi) return true;
-    for (int i = 0; i < known; ++i)
-      for (int j = 0; j < streams[i].count; ++j) {
-        const Range& r = streams[i].range[j];
-        if (lo < r.hi && r.lo < hi && streams[i].live(r)) return true;
-      }
+    const Range& kept = rest[capture != 0];
+    if (lo < kept.hi && kept.lo < hi) return true;
+    for (int i = 0; i < known; ++i) {
+      const Stream& s = streams[i];
+      if (s.key.capture != capture) continue;
+      for (int j = 0; j < s.count; ++j)
+        if (lo < s.range[j].hi && s.range[j].lo < hi && s.live(s.range[j])) return true;
+    }
     return false;
   }
 };
 inline OutputRecord g_outputs;
 
-inline void note_launch(cudaStream_t st) { g_outputs.launched(st); }
-inline void note_outputs(cudaStream_t st, std::initializer_list<Output> outputs) { g_outputs.wrote(st, outputs); }
+inline void note_launch(cudaStream_t st) { g_outputs.launched(stream_key(st)); }
+inline void note_outputs(cudaStream_t st, std::initializer_list<Output> outputs, int launches = 0) { g_outputs.wrote(stream_key(st), outputs, launches); }
 
-inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes) {
+// Whether a call on stream st may find an output in flight in a tensor.
+inline bool overlaps_recent_output(const pkv_tensor& t, int batch, int heads, int tokens, int d, int elem_bytes, cudaStream_t st) {
   const int64_t last = (batch - 1) * std::max<int64_t>(t.stride_batch, 0) +
                        (heads - 1) * std::max<int64_t>(t.stride_head, 0) + (tokens - 1) * t.stride_token + d;
   const uintptr_t lo = reinterpret_cast<uintptr_t>(t.ptr), hi = lo + static_cast<uintptr_t>(last) * elem_bytes;
-  return g_outputs.overlaps(lo, hi);
+  return g_outputs.overlaps(stream_key(st).capture, lo, hi);
 }
 
 // Launch with programmatic stream serialisation: the kernel may be scheduled while its predecessor in
 // the stream drains; the kernels order themselves with pdl_wait() (pkv_common.cuh).
 template <typename... KArgs, typename... Args>
-void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+bool launch_uncounted(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
@@ -176,7 +198,11 @@ void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cu
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) == cudaSuccess) note_launch(st);
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...) == cudaSuccess;
+}
+template <typename... KArgs, typename... Args>
+void launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args) {
+  if (launch_uncounted(kernel, grid, block, smem, st, std::forward<Args>(args)...)) note_launch(st);
 }
 
 // SMs the persistent score kernels may count on: the device's, or fewer while a call runs them on a lane that

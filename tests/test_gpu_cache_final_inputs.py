@@ -1,5 +1,5 @@
 """Scores of inputs that the caller calls final: what calls of the library are still to write is waited for, however many other calls
-of the library come between or run on another stream."""
+of the library come between, run on another stream or are captured meanwhile."""
 import pytest
 import torch
 
@@ -24,7 +24,7 @@ class Decoding:
         pkv.append_cache(self.x.cfg, self.x.cache, 0, self.positions, self.k, self.k, self.x.ws, q=self.q, q_out=self.q_out, rotary=self.plan, stream=stream)
 
 
-@pytest.mark.parametrize("where,calls", [("same stream", 90), ("other stream", 90), ("other stream", 400), ("none", 0)])
+@pytest.mark.parametrize("where,calls", [("same stream", 90), ("other stream", 90), ("other stream", 400), ("captured", 200), ("none", 0)])
 def test_scores_wait_for_the_rotation_behind_many_appends(where, calls):
     cfg = pkv.make_config(num_layers=2, num_q_heads=4, num_kv_heads=1, head_dim=128, window=8, pool_kernel=5, dtype="bf16", avg_budget=24, inputs_final=True)
     n = 300                                                          # (few CTAs of the rotation, so that the scores find room beside it)
@@ -36,19 +36,25 @@ def test_scores_wait_for_the_rotation_behind_many_appends(where, calls):
     ws = pkv.new_workspace(cfg, 1, n, DEV)
     rows = pkv.total_rows(cfg, pkv.layer_budgets(cfg)[0], [n])
     filler, slow = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV), torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
-    decoding, side = Decoding(), torch.cuda.Stream()
+    decoding, main, side = Decoding(), torch.cuda.Stream(), torch.cuda.Stream()
 
     def step(held):
         qr.copy_(q)
         kr.copy_(k)
         out = [torch.zeros(rows, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)] + [torch.zeros(rows, dtype=torch.int32, device=DEV)]
         torch.cuda.synchronize()
-        if held:
-            binding.slow_copy(slow, filler, steps=2048)              # lets the calls behind it start at once
-        pkv.rotary(cfg, plan, positions, qr, kr)
-        for _ in range(calls if held else 0):
-            decoding.append(side if where == "other stream" else None)
-        pkv.compress_layer(cfg, 0, qr[:, :, n - 8:], kr, v, [n], out[0], out[1], out[2], ws)
+        with torch.cuda.stream(main):
+            if held:
+                binding.slow_copy(slow, filler, steps=2048)          # lets the calls behind it start at once
+            pkv.rotary(cfg, plan, positions, qr, kr)
+            if held and where == "captured":                         # (nothing of it runs)
+                graph = torch.cuda.CUDAGraph()
+                graph.capture_begin(capture_error_mode="thread_local")
+            for _ in range(calls if held else 0):
+                decoding.append(side if where == "other stream" else None)
+            if held and where == "captured":
+                graph.capture_end()
+            pkv.compress_layer(cfg, 0, qr[:, :, n - 8:], kr, v, [n], out[0], out[1], out[2], ws)
         torch.cuda.synchronize()
         return out
     want = step(False)

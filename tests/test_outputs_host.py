@@ -12,14 +12,15 @@ SOURCE = r"""
 #include "pkv_host.cuh"
 using namespace pkv;
 static int failed = 0;
-static cudaStream_t stream(uintptr_t i) { return reinterpret_cast<cudaStream_t>(0x100000 + 64 * i); }
+static StreamKey stream(uintptr_t i, uint64_t capture = 0) { return StreamKey{reinterpret_cast<cudaStream_t>(0x100000 + 64 * i), -1, 0, capture}; }
 static void* at(uintptr_t a) { return reinterpret_cast<void*>(a); }
-static bool known(uintptr_t lo, uintptr_t hi) { return g_outputs.overlaps(lo, hi); }
+static bool known(uintptr_t lo, uintptr_t hi, uint64_t capture = 0) { return g_outputs.overlaps(capture, lo, hi); }
 static void want(bool ok, const char* what) { if (!ok) { std::printf("%s\n", what); failed = 1; } }
-static void note_output(const void* p, size_t n, cudaStream_t st) { note_outputs(st, {{p, n}}); }
-static void launch(cudaStream_t st, int n = 1) { for (int i = 0; i < n; ++i) note_launch(st); }
+static void note_launch(const StreamKey& k) { g_outputs.launched(k); }
+static void note_output(const void* p, size_t n, const StreamKey& k) { g_outputs.wrote(k, {{p, n}}); }
+static void launch(const StreamKey& k, int n = 1) { for (int i = 0; i < n; ++i) note_launch(k); }
 int main() {
-  const cudaStream_t a = stream(1), b = stream(2);
+  const StreamKey a = stream(1), b = stream(2);
   note_launch(a);
   note_output(at(0x10000), 0x100, a);
   want(known(0x10000, 0x10001) && known(0x100ff, 0x20000) && known(0, 0x10001), "an output is known");
@@ -52,6 +53,20 @@ int main() {
   note_output(at(0x50000), 0x1000, a);
   launch(a, 100);
   want(known(0x50000, 0x50001) && known(0x50fff, 0x51000), "the whole again");
+  // captures: launches that are captured are not behind anything that runs, and a capture looks at its own outputs only
+  note_launch(a);
+  note_output(at(0x60000), 0x100, a);
+  launch(stream(1, 7), 500);
+  want(known(0x60000, 0x60100), "captured launches are not behind it");
+  note_output(at(0x68000), 0x100, stream(1, 7));
+  note_launch(stream(2, 7));
+  note_output(at(0x69000), 0x100, stream(2, 7));
+  want(known(0x68000, 0x68100, 7) && known(0x69000, 0x69100, 7), "outputs of a capture, on both of its streams");
+  want(!known(0x68000, 0x69100) && !known(0x68000, 0x69100, 8) && !known(0x60000, 0x60100, 7), "are nobody else's");
+  note_launch(stream(1, 8));
+  want(!known(0x68000, 0x68100, 8) && known(0x69000, 0x69100, 7), "another capture on the stream starts with nothing");
+  launch(a, 128);
+  want(!known(0x60000, 0x60100), "launches that run are");
   // more streams than there is room for: nothing is lost
   for (uintptr_t s = 10; s < 300; ++s) {
     note_launch(stream(s));
